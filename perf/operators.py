@@ -101,10 +101,12 @@ def _settings(filters, n, g):
 
 
 def _logits(rows, vocab, g, masked):
-    """Rows as a language model's head gives them: a broad bulk, some forty tokens that fit.  Every fifth row sits on the
-    grid of bf16, as a head of that type leaves it; where masked, every seventh has nine tenths forbidden."""
-    x = torch.randn(rows, vocab, generator=g, device="cuda") * 2.2
-    x += 7.0 * (torch.rand(rows, vocab, generator=g, device="cuda") < 40.0 / vocab)
+    """Rows as a language model's head gives them: a broad bulk and some forty tokens that fit, by a lead that goes from
+    none to speak of (an open choice of thousands of tokens) to certainty.  Every fifth row sits on the grid of bf16, as a
+    head of that type leaves it; where masked, every seventh has nine tenths forbidden."""
+    x = torch.randn(rows, vocab, generator=g, device="cuda") * 1.8
+    lead = 8.0 + 10.0 * torch.rand(rows, 1, generator=g, device="cuda")
+    x += lead * (torch.rand(rows, vocab, generator=g, device="cuda") < 40.0 / vocab)
     row = torch.arange(rows, device="cuda")
     x = torch.where((row % 5 == 1)[:, None], x.to(torch.bfloat16).float(), x)
     if masked:

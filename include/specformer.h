@@ -335,6 +335,58 @@ sf_status sf_op_accept(const sf_ctx *ctx, int32_t B, int32_t k, const int32_t *d
                        int32_t *out_tokens, int32_t *kv_len, int32_t *pending, int32_t *n_new, int32_t *cu_new,
                        void *stream);
 
+/* ---- sampled decoding (temperature > 0) ------------------------------------------------------
+ * Settings of the rows of one call, each array dev [entries] or NULL (off).  A row's tokens are ranked by falling logit,
+ * equal logits by rising index; NaN is no token.  With M the row's largest logit, w_i = exp((l_i - M) / temperature):
+ *   temperature  default 1; <= 0 or NaN: greedy, the first of the ranking alone (what sf_op_argmax returns)
+ *   top_k        the k first of the ranking stay; <= 0: all
+ *   top_p        of those, the ones in front of which less than top_p of their weight lies; >= 1 or NaN: all
+ *   min_p        of those, the ones with w_i >= min_p; <= 0 or NaN: all
+ * The first of the ranking always stays; -inf has weight 0.  A token is drawn by a number u in [0, 1): the first, by index,
+ * whose running kept weight exceeds u times the kept weight (u outside [0, 1) counts as the nearest border, NaN as the
+ * upper one).  Weights and sums are doubles and their order is fixed: the same call returns the same bits. */
+typedef struct {
+  const float *temperature;
+  const int32_t *top_k;
+  const float *top_p;
+  const float *min_p;
+} sf_sampling;
+
+/* ids[r] = the token drawn from row r of logits (dev float [M][V], any alignment of 4 bytes) by u[r].  Row r goes by entry
+ * r / group of the settings (sampling: host struct, NULL: all off).  prob: dev float [M] or NULL, the drawn token's share of
+ * the kept weight.  dist: dev, sf_sample_dist_bytes(M) bytes, 8-byte aligned, or NULL: what is kept of every row, for
+ * sf_op_accept_sampled.  A row without any comparable value gives id 0 and prob 0.  M, V <= 2^20 (SF_EUNSUPPORTED beyond).
+ * workspace: dev, 256-byte aligned, sf_sample_workspace_bytes; nothing is kept in it between calls. */
+size_t sf_sample_workspace_bytes(int32_t M, int32_t V);
+size_t sf_sample_dist_bytes(int32_t M);
+sf_status sf_op_sample(const sf_ctx *ctx, const float *logits, int32_t M, int32_t V, int32_t group,
+                       const sf_sampling *sampling, const float *u, int32_t *ids, float *prob, void *dist,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/* Multi-token acceptance at temperature > 0, lossless in distribution: with p_i the kept distribution of the target's logits
+ * at block row i and q_i the one that slot i's token d was drawn from, slot i is accepted if all before it are and
+ *   u_accept[b][i] * q_i(d) < p_i(d);
+ * behind the n accepted slots a token is drawn from max(p_n - q_n, 0) by u_sample[b] (n == k: from p_k).  Then the block is
+ * committed as by sf_op_accept: accept_len[b] = n + 1, out_tokens[b] = the accepted slots, the drawn token, -1 behind.
+ *   target_logits  dev float [B][k+1][V], as sf_verify_step stores them; sampling: one entry per sequence
+ *   draft_logits   dev float [B][k][V] with draft_dist, what sf_op_sample left for these B*k rows (with settings of its own);
+ *                  NULL: the draft is certain of its tokens (greedy drafts), q_i(d) = 1
+ *   u_accept       dev [B][k]; u_sample: dev [B]; all in [0, 1)
+ * A drafted id outside [0, V) is not accepted.  At temperature 0 this is sf_op_accept on the target's greedy choices.
+ * Other arguments as sf_op_accept.  workspace: dev, 256-byte aligned, sf_accept_sampled_workspace_bytes. */
+size_t sf_accept_sampled_workspace_bytes(int32_t B, int32_t k, int32_t V);
+sf_status sf_op_accept_sampled(const sf_ctx *ctx, int32_t B, int32_t k, int32_t V, const int32_t *draft_tokens,
+                               const float *target_logits, const sf_sampling *sampling, const float *draft_logits,
+                               const void *draft_dist, const float *u_accept, const float *u_sample, int32_t *accept_len,
+                               int32_t *out_tokens, int32_t *kv_len, int32_t *pending, int32_t *n_new, int32_t *cu_new,
+                               void *workspace, size_t workspace_bytes, void *stream);
+/* The same on a state: what sf_accept_commit is to sf_op_accept, with its order of calls (SF_ESTATE). */
+sf_status sf_accept_commit_sampled(sf_ctx *ctx, const sf_state *st, int32_t k, const int32_t *draft_tokens,
+                                   const float *target_logits, const sf_sampling *sampling, const float *draft_logits,
+                                   const void *draft_dist, const float *u_accept, const float *u_sample,
+                                   int32_t *accept_len, int32_t *out_tokens, void *workspace, size_t workspace_bytes,
+                                   void *stream);
+
 const char *sf_strerror(sf_status s);
 /* HIP error code (hipError_t) of the last SF_EHIP on this context, 0 if none. host. */
 int sf_last_hip_error(const sf_ctx *ctx);

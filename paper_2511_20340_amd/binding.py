@@ -22,6 +22,8 @@ EXPORTS = [
     "sf_op_rmsnorm_linear", "sf_op_linear_swiglu", "sf_linear_argmax_workspace_bytes", "sf_op_linear_argmax",
     "sf_op_rmsnorm", "sf_op_rope_kv_append", "sf_rope_attention_workspace_bytes", "sf_op_rope_attention",
     "sf_op_silu_mul", "sf_argmax_workspace_bytes", "sf_op_argmax", "sf_op_argmax_noalloc", "sf_op_accept", "sf_strerror",
+    "sf_sample_workspace_bytes", "sf_sample_dist_bytes", "sf_op_sample", "sf_accept_sampled_workspace_bytes",
+    "sf_op_accept_sampled", "sf_accept_commit_sampled",
     "sf_last_hip_error", "sf_version",
     # include/specformer_aux.h
     "sf_tune_linear", "sf_linear_num_tiles", "sf_linear_config", "sf_linear_choice", "sf_tune_attention", "sf_calib_copy",
@@ -50,6 +52,10 @@ class State(C.Structure):
     _fields_ = [("B", i32), ("cap", i32), ("tk", vp), ("tv", vp), ("dk", vp), ("dv", vp), ("kv_len", vp),
                 ("pending", vp), ("hooks", vp), ("n_new", vp), ("cu_new", vp), ("workspace", vp),
                 ("workspace_bytes", sz)]
+
+
+class Sampling(C.Structure):
+    _fields_ = [(n, vp) for n in ("temperature", "top_k", "top_p", "min_p")]
 
 
 class SfError(RuntimeError):
@@ -121,6 +127,16 @@ def lib():
     L.sf_argmax_workspace_bytes.restype = sz
     L.sf_op_argmax.argtypes = [vp, vp, i32, i32, vp, vp, sz, vp]
     L.sf_op_argmax_noalloc.argtypes = [vp, vp, i32, i32, vp, vp]
+    L.sf_sample_workspace_bytes.argtypes = [i32, i32]
+    L.sf_sample_workspace_bytes.restype = sz
+    L.sf_sample_dist_bytes.argtypes = [i32]
+    L.sf_sample_dist_bytes.restype = sz
+    L.sf_op_sample.argtypes = [vp, vp, i32, i32, i32, P(Sampling), vp, vp, vp, vp, vp, sz, vp]
+    L.sf_accept_sampled_workspace_bytes.argtypes = [i32, i32, i32]
+    L.sf_accept_sampled_workspace_bytes.restype = sz
+    L.sf_op_accept_sampled.argtypes = [vp, i32, i32, i32, vp, vp, P(Sampling), vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz,
+                                       vp]
+    L.sf_accept_commit_sampled.argtypes = [vp, P(State), i32, vp, vp, P(Sampling), vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.sf_calib_copy.argtypes = [vp, vp, sz, vp]
     L.sf_profile_begin.argtypes = [vp]
     L.sf_profile_end.argtypes = [vp, P(C.c_double), P(i32), i32]

@@ -881,6 +881,125 @@ sf_status sf_op_argmax_noalloc(const sf_ctx *c, const float *logits, int32_t M, 
   return SF_OK;
 }
 
+namespace {
+
+// accept workspace: the target rows' distributions, segment sums, the block's tokens and their number
+struct AcceptPlan {
+  size_t dist, part, tokens, accept, sample, total;
+};
+AcceptPlan accept_plan(int B, int k, int V) {
+  const size_t rows = (size_t)B * (k + 1), segs = ((size_t)V + SAMPLE_SEG - 1) / SAMPLE_SEG;
+  AcceptPlan p;
+  size_t off = 0;
+  auto take = [&](size_t bytes) { size_t o = off; off += up(bytes); return o; };
+  p.dist = take(rows * sizeof(SampleDist));
+  p.part = take((size_t)B * segs * sizeof(double));
+  p.tokens = take(rows * sizeof(int32_t));
+  p.accept = take((size_t)B * sizeof(int32_t));
+  p.total = off;
+  return p;
+}
+
+struct AcceptSampled {
+  const int32_t *draft;
+  const float *target_logits;
+  const sf_sampling *par;
+  const float *draft_logits;
+  const void *draft_dist;
+  const float *u_accept, *u_sample;
+  void *workspace;
+  size_t workspace_bytes;
+};
+
+sf_status check_accept_sampled(int B, int k, int V, const AcceptSampled &s) {
+  if (B < 1 || k < 0 || k > 127 || V < 1) return SF_EINVAL;
+  if (!s.target_logits || !s.u_sample || !s.workspace) return SF_EINVAL;
+  if (k > 0 && (!s.draft || !s.u_accept || (s.draft_logits && !s.draft_dist))) return SF_EINVAL;
+  if (k > 0 && s.draft_logits && ((uintptr_t)s.draft_dist) % alignof(SampleDist)) return SF_EINVAL;
+  if (((uintptr_t)s.workspace) % ALIGN) return SF_EINVAL;
+  const long rows = (long)B * (k + 1), segs = ((long)V + SAMPLE_SEG - 1) / SAMPLE_SEG;
+  if (V > SAMPLE_MAX_VOCAB || rows > SAMPLE_MAX_ROWS || B * segs > INT32_MAX) return SF_EUNSUPPORTED;
+  return s.workspace_bytes < accept_plan(B, k, V).total ? SF_ECAPACITY : SF_OK;
+}
+
+// the target rows' distributions, the acceptance and the drawn token, then the commit of the block's tokens by their number
+void accept_sampled(Run &r, int B, int k, int V, const AcceptSampled &s, int32_t *accept_len, int32_t *out_tokens,
+                    int32_t *kv_len, int32_t *pending, int32_t *n_new, int32_t *cu_new) {
+  const AcceptPlan p = accept_plan(B, k, V);
+  char *ws = (char *)s.workspace;
+  const sf_sampling none{};
+  const sf_sampling &par = s.par ? *s.par : none;
+  SampleDist *dist = (SampleDist *)(ws + p.dist);
+  SampleArgs a{s.target_logits, B * (k + 1), V, k + 1, par.temperature, par.top_k, par.top_p, par.min_p,
+               nullptr, nullptr, nullptr, dist};
+  LAUNCH(K_ARGMAX, launch_sample(a, r.s));
+  SampleAcceptArgs c{s.draft, s.target_logits, dist, k > 0 ? s.draft_logits : nullptr, (const SampleDist *)s.draft_dist,
+                     s.u_accept, s.u_sample, (double *)(ws + p.part), (int32_t *)(ws + p.tokens),
+                     (int32_t *)(ws + p.accept), B, k, V};
+  LAUNCH(K_ACCEPT, launch_sample_accept(c, r.s));
+  AcceptArgs e{c.tokens, nullptr, c.accept, accept_len, out_tokens, kv_len, pending, n_new, cu_new, B, k};
+  LAUNCH(K_ACCEPT, launch_accept(e, r.s));
+}
+
+}  // namespace
+
+size_t sf_sample_dist_bytes(int32_t M) { return M < 1 ? 0 : (size_t)M * sizeof(SampleDist); }
+
+size_t sf_sample_workspace_bytes(int32_t M, int32_t V) {
+  (void)M; (void)V;
+  return 0;
+}
+
+sf_status sf_op_sample(const sf_ctx *c, const float *logits, int32_t M, int32_t V, int32_t group, const sf_sampling *par,
+                       const float *u, int32_t *ids, float *prob, void *dist, void *workspace, size_t workspace_bytes,
+                       void *stream) {
+  if (!c || !logits || !u || !ids || M < 1 || V < 1 || group < 1) return SF_EINVAL;
+  if (((uintptr_t)dist) % alignof(SampleDist)) return SF_EINVAL;
+  if (V > SAMPLE_MAX_VOCAB || M > SAMPLE_MAX_ROWS) return SF_EUNSUPPORTED;
+  const size_t need = sf_sample_workspace_bytes(M, V);
+  if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace) % ALIGN)) return SF_ECAPACITY;
+  const sf_sampling none{};
+  if (!par) par = &none;
+  SampleArgs a{logits, M, V, group, par->temperature, par->top_k, par->top_p, par->min_p, u, ids, prob, (SampleDist *)dist};
+  Run r{c, (hipStream_t)stream};
+  LAUNCH(K_ARGMAX, launch_sample(a, r.s));
+  return r.st;
+}
+
+size_t sf_accept_sampled_workspace_bytes(int32_t B, int32_t k, int32_t V) {
+  return B < 1 || k < 0 || k > 127 || V < 1 ? 0 : accept_plan(B, k, V).total;
+}
+
+sf_status sf_op_accept_sampled(const sf_ctx *c, int32_t B, int32_t k, int32_t V, const int32_t *draft,
+                               const float *target_logits, const sf_sampling *par, const float *draft_logits,
+                               const void *draft_dist, const float *u_accept, const float *u_sample, int32_t *accept_len,
+                               int32_t *out_tokens, int32_t *kv_len, int32_t *pending, int32_t *n_new, int32_t *cu_new,
+                               void *workspace, size_t workspace_bytes, void *stream) {
+  if (!c || !accept_len || !out_tokens || !kv_len || !pending || !n_new || !cu_new) return SF_EINVAL;
+  const AcceptSampled s{draft, target_logits, par, draft_logits, draft_dist, u_accept, u_sample, workspace, workspace_bytes};
+  const sf_status v = check_accept_sampled(B, k, V, s);
+  if (v != SF_OK) return v;
+  Run r{c, (hipStream_t)stream};
+  accept_sampled(r, B, k, V, s, accept_len, out_tokens, kv_len, pending, n_new, cu_new);
+  return r.st;
+}
+
+sf_status sf_accept_commit_sampled(sf_ctx *c, const sf_state *st, int32_t k, const int32_t *draft, const float *target_logits,
+                                   const sf_sampling *par, const float *draft_logits, const void *draft_dist,
+                                   const float *u_accept, const float *u_sample, int32_t *accept_len, int32_t *out_tokens,
+                                   void *workspace, size_t workspace_bytes, void *stream) {
+  sf_status v = check_state(c, st, k, false);
+  if (v != SF_OK) return v;
+  if (!accept_len || !out_tokens) return SF_EINVAL;
+  const AcceptSampled s{draft, target_logits, par, draft_logits, draft_dist, u_accept, u_sample, workspace, workspace_bytes};
+  if ((v = check_accept_sampled(st->B, k, c->tc.vocab, s)) != SF_OK) return v;
+  if (c->verified_state != st->kv_len || c->verified_k != k) return SF_ESTATE;
+  Run r{c, (hipStream_t)stream};
+  accept_sampled(r, st->B, k, c->tc.vocab, s, accept_len, out_tokens, st->kv_len, st->pending, st->n_new, st->cu_new);
+  if (r.st == SF_OK) { c->verified_state = nullptr; c->verified_k = -1; }
+  return r.st;
+}
+
 sf_status sf_calib_copy(void *dst, const void *src, size_t bytes, void *stream) {
   if (!dst || !src || bytes % 16 || (((uintptr_t)dst | (uintptr_t)src) % 16)) return SF_EINVAL;
   return launch_calib_copy(src, dst, bytes, (hipStream_t)stream) == hipSuccess ? SF_OK : SF_EHIP;

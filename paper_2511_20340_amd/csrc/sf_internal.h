@@ -226,4 +226,43 @@ struct AcceptArgs {
 };
 hipError_t launch_accept(const AcceptArgs &a, hipStream_t s);
 
+// ---- sampling (sample.hip) --------------------------------------------------------------------
+constexpr int SAMPLE_MAX_VOCAB = 1 << 20, SAMPLE_MAX_ROWS = 1 << 20;
+constexpr int SAMPLE_SEG = 8192;  // tokens of a row that one workgroup sums; 256 threads hold a row's segments
+static_assert(SAMPLE_MAX_VOCAB / SAMPLE_SEG <= 256 && SAMPLE_SEG / 64 <= 256, "one thread per segment, one per step of a segment");
+// What is kept of a row: the tokens with l > thr, or l == thr and an index <= last; their weights exp((l - top) / temp) sum
+// up to z.  id, prob: the token drawn.
+struct SampleDist {
+  float top, thr;
+  int32_t last;
+  float temp;
+  double z;
+  int32_t id;
+  float prob;
+};
+struct SampleArgs {
+  const float *logits;  // [M][V]
+  int M, V, group;      // row r goes by entry r / group of the settings
+  const float *temperature;
+  const int32_t *top_k;
+  const float *top_p, *min_p;
+  const float *u;    // [M]
+  int32_t *ids;      // each optional
+  float *prob;
+  SampleDist *dist;
+};
+hipError_t launch_sample(const SampleArgs &a, hipStream_t s);
+struct SampleAcceptArgs {
+  const int32_t *draft;       // [B][k]
+  const float *target;        // [B][k+1][V]
+  const SampleDist *dist;     // [B][k+1]
+  const float *draft_logits;  // [B][k][V] or null
+  const SampleDist *draft_dist;
+  const float *u_accept, *u_sample;
+  double *part;               // [B][segments]
+  int32_t *tokens, *accept;   // [B][k+1]: drafted ones, then the drawn one; [B]: their number
+  int B, k, V;
+};
+hipError_t launch_sample_accept(const SampleAcceptArgs &a, hipStream_t s);
+
 }  // namespace sf

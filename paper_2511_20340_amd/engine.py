@@ -426,6 +426,113 @@ class Engine:
                   "sf_op_argmax_noalloc", self.ctx)
         return ids
 
+    # ---- sampled decoding --------------------------------------------------------------------
+    def _need(self, what, name, t, shape, dtype):
+        """t is a dense tensor of that shape and type on the engine's device."""
+        if not isinstance(t, torch.Tensor) or tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+            raise ValueError(f"{what}: {name} must be a dense {dtype} tensor of shape {tuple(shape)}")
+        if t.device != self._cuda_dev():
+            raise ValueError(f"{what}: {name} is on {t.device}, the engine on {self._cuda_dev()}")
+
+    def _cuda_dev(self):
+        return self.dev if self.dev.index is not None else torch.device("cuda", torch.cuda.current_device())
+
+    def _sampling(self, what, n, temperature, top_k, top_p, min_p):
+        s = sfb.Sampling()
+        for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
+                               ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
+            if t is not None:
+                self._need(what, name, t, (n,), dtype)
+                setattr(s, name, t.data_ptr())
+        return s
+
+    def _workspace(self, nbytes):
+        """(tensor, aligned pointer) of a call's workspace, from the allocator of the current stream."""
+        ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.dev)
+        return ws, C.c_void_p(ws.data_ptr() + (-ws.data_ptr()) % 256)
+
+    def sf_op_sample(self, logits, u, temperature=None, top_k=None, top_p=None, min_p=None, group=1, want_prob=False,
+                     want_dist=False, ids=None):
+        """Tokens drawn from logits [M,V] (float32) by u [M]; settings: device tensors [ceil(M/group)] or None (off), row r goes
+        by entry r // group.  -> ids [M] int32, then the drawn tokens' probabilities [M] if want_prob, then what
+        sf_op_accept_sampled takes as draft_dist if want_dist."""
+        what = "sf_op_sample"
+        if logits.dim() != 2 or group < 1:
+            raise ValueError(f"{what}: logits must be [M,V], group >= 1")
+        M, V = logits.shape
+        self._need(what, "logits", logits, (M, V), torch.float32)
+        self._need(what, "u", u, (M,), torch.float32)
+        par = self._sampling(what, -(-M // group), temperature, top_k, top_p, min_p)
+        if ids is not None:
+            self._need(what, "ids", ids, (M,), torch.int32)
+        with torch.cuda.device(self.dev):
+            if ids is None:
+                ids = torch.empty(M, dtype=torch.int32, device=self.dev)
+            prob = torch.empty(M, dtype=torch.float32, device=self.dev) if want_prob else None
+            dist = torch.empty(self.lib.sf_sample_dist_bytes(M), dtype=torch.uint8, device=self.dev) if want_dist else None
+            nb = self.lib.sf_sample_workspace_bytes(M, V)
+            ws, p = self._workspace(nb)
+            sfb.check(self.lib.sf_op_sample(self.ctx, _ptr(logits), M, V, group, C.byref(par), _ptr(u), _ptr(ids), _ptr(prob),
+                                            _ptr(dist), p, nb, _stream()), what, self.ctx)
+        out = (ids,) + ((prob,) if want_prob else ()) + ((dist,) if want_dist else ())
+        return out if len(out) > 1 else ids
+
+    def _accept_sampled(self, what, call, k, V, draft, target_logits, u_accept, u_sample, settings, draft_logits, draft_dist,
+                        accept_out, tokens_out):
+        B, i32, f32 = self.B, torch.int32, torch.float32
+        self._need(what, "target_logits", target_logits, (B, k + 1, V), f32)
+        self._need(what, "u_sample", u_sample, (B,), f32)
+        if k > 0:
+            self._need(what, "draft", draft, (B, k), i32)
+            self._need(what, "u_accept", u_accept, (B, k), f32)
+            if (draft_logits is None) != (draft_dist is None):
+                raise ValueError(f"{what}: draft_logits and draft_dist come together")
+            if draft_logits is not None:
+                self._need(what, "draft_logits", draft_logits, (B, k, V), f32)
+                self._need(what, "draft_dist", draft_dist, (self.lib.sf_sample_dist_bytes(B * k),), torch.uint8)
+        else:
+            draft = u_accept = draft_logits = draft_dist = None
+        par = self._sampling(what, B, *settings)
+        if accept_out is not None:
+            self._need(what, "accept_out", accept_out, (B,), i32)
+        if tokens_out is not None:
+            self._need(what, "tokens_out", tokens_out, (B, k + 1), i32)
+        with torch.cuda.device(self.dev):
+            acc = accept_out if accept_out is not None else torch.empty(B, dtype=i32, device=self.dev)
+            out = tokens_out if tokens_out is not None else torch.empty(B, k + 1, dtype=i32, device=self.dev)
+            nb = self.lib.sf_accept_sampled_workspace_bytes(B, k, V)
+            ws, p = self._workspace(nb)
+            sfb.check(call(_ptr(draft), _ptr(target_logits), C.byref(par), _ptr(draft_logits), _ptr(draft_dist),
+                           _ptr(u_accept), _ptr(u_sample), acc, out, p, nb), what, self.ctx)
+        return acc, out
+
+    def sf_op_accept_sampled(self, k, draft, target_logits, u_accept, u_sample, temperature=None, top_k=None, top_p=None,
+                             min_p=None, draft_logits=None, draft_dist=None):
+        """The acceptance rule at temperature > 0 alone, on this engine's state arrays (no call-order check).  target_logits
+        [B,k+1,V], draft [B,k], u_accept [B,k], u_sample [B], settings [B]; draft_logits [B,k,V] with the draft_dist that
+        sf_op_sample left for them, or neither for greedy drafts.  -> (accept_len [B], out_tokens [B,k+1])"""
+        V = target_logits.shape[-1]
+
+        def call(d, t, par, dl, dd, ua, us, acc, out, ws, nb):
+            return self.lib.sf_op_accept_sampled(self.ctx, self.B, k, V, d, t, par, dl, dd, ua, us, _ptr(acc), _ptr(out),
+                                                 _ptr(self.kv_len), _ptr(self.pending), _ptr(self.n_new), _ptr(self.cu_new),
+                                                 ws, nb, _stream())
+        return self._accept_sampled("sf_op_accept_sampled", call, k, V, draft, target_logits, u_accept, u_sample,
+                                    (temperature, top_k, top_p, min_p), draft_logits, draft_dist, None, None)
+
+    def sf_accept_commit_sampled(self, k, draft, target_logits, u_accept, u_sample, temperature=None, top_k=None, top_p=None,
+                                 min_p=None, draft_logits=None, draft_dist=None, accept_out=None, tokens_out=None):
+        """sf_accept_commit at temperature > 0: arguments as sf_op_accept_sampled, target_logits as sf_verify_step returned
+        them."""
+        def call(d, t, par, dl, dd, ua, us, acc, out, ws, nb):
+            return self.lib.sf_accept_commit_sampled(self.ctx, C.byref(self.st), k, d, t, par, dl, dd, ua, us, _ptr(acc),
+                                                     _ptr(out), ws, nb, _stream())
+        r = self._accept_sampled("sf_accept_commit_sampled", call, k, self.V, draft, target_logits, u_accept, u_sample,
+                                 (temperature, top_k, top_p, min_p), draft_logits, draft_dist, accept_out, tokens_out)
+        if not self._pinned:
+            self.len_upper = min(self.len_upper + k + 1, self.cap)
+        return r
+
     # ---- prefill: chunked verify with forced acceptance --------------------------------------
     def prefill(self, prompts, block=None):
         """Feeds every prompt through the target in blocks of `block` tokens (default max_k+1) with forced commits,

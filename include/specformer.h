@@ -218,6 +218,24 @@ sf_status sf_op_attention(const sf_ctx *ctx, const void *q, const void *kc, cons
                           int32_t host_len_upper, void *out, void *workspace, size_t workspace_bytes,
                           void *stream);
 
+/* Attention of a batch whose sequences all continue one shared prefix (several continuations of one prompt): row (b,i) sees
+ * the prefix's keys [0, prefix_len), then what sf_op_attention would show it.  The prefix is read once for the rows of all
+ * sequences, not once per sequence.
+ *   pk, pv      one layer's tiled caches of ONE sequence of capacity prefix_cap (multiple of 32), the slab that a state of
+ *               B = 1 has; read only, what lies behind prefix_len is not looked at.  prefix_len: host, 0: sf_op_attention
+ *   kc, vc      the sequences' own caches: positions behind the prefix, own key j of sequence b at slot j; kv_len[b] own keys
+ *               (without the prefix's), then the block's n_q
+ * Rotations are the caller's: a row's position is prefix_len + kv_len[b] + i.  All pointers 16-byte aligned; B < 2^16, B * n_q <= 2^20,
+ * a kv head's slab of the prefix below 4 GiB (SF_EUNSUPPORTED beyond).  Other arguments as sf_op_attention; workspace: dev,
+ * 256-byte aligned, sf_prefix_attention_workspace_bytes; nothing is kept in it between calls. */
+enum { SF_PREFIX_MAX_ROWS = 1 << 20 };
+size_t sf_prefix_attention_workspace_bytes(const sf_ctx *ctx, int32_t B, int32_t n_q, int32_t prefix_len,
+                                           int32_t host_len_upper);
+sf_status sf_op_prefix_attention(const sf_ctx *ctx, const void *q, const void *pk, const void *pv, int32_t prefix_len,
+                                 int32_t prefix_cap, const void *kc, const void *vc, const int32_t *kv_len, int32_t B,
+                                 int32_t n_q, int32_t cap, int32_t mask, int32_t host_len_upper, void *out, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+
 /* Weight packing.  w: dev elem row-major [N][K]; packed: dev, sf_packed_weight_bytes(ctx,N,K) bytes,
  * 16-byte aligned.  bf16: 32-row x 16-column units of 1 KiB in the lane order of the 32x32x16 MFMA,
  * rows and columns zero-padded to multiples of 32 / 16; a prefix of whole 32-row blocks of a packed

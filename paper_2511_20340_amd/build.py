@@ -8,7 +8,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libspecformer.so")
-SOURCES = ["api.hip", "attention.hip", "gemm.hip", "gemm_tiles_narrow.hip",
+SOURCES = ["api.hip", "attention.hip", "attention_prefix.hip", "gemm.hip", "gemm_tiles_narrow.hip",
            "gemm_tiles_wide.hip", "gemm_tiles_tall.hip", "gemm_stream.hip", "gemm_block.hip", "gemm_panel.hip",
            "gemm_panel_narrow.hip", "gemm_f32.hip", "elementwise.hip", "accept.hip", "sample.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -265,6 +265,49 @@ void attention(Run &r, const sf_model_cfg &m, const void *q, const void *kc, con
   if (m.dtype == SF_BF16 && a.n_chunks > 1) LAUNCH(K_ATTN_COMBINE, launch_attention_combine(a, r.s));
 }
 
+// The same over a shared prefix in front of every sequence.  ws: prefix_ws_bytes.
+struct Prefix {
+  const void *k, *v;
+  int len, cap;
+  void *ws;
+};
+// floats of the partials: the prefix's rows x chunks, then the own ones (a partial of every chunk), hd + 2 each
+size_t prefix_ws_rows(const sf_model_cfg &m, int B, int n_q, int prefix_len, int len_upper, size_t *own) {
+  const PrefixPlan p = prefix_plan(B, n_q, m.n_q_heads, m.n_kv_heads, prefix_len);
+  const size_t n_rt = (m.n_q_heads / m.n_kv_heads * n_q + 31) / 32, n_tiles = ((size_t)len_upper + n_q + TK - 1) / TK;
+  *own = (size_t)B * m.n_kv_heads * ((n_tiles + 15) / 16) * n_rt * 32;  // chunks have 16 tiles at least
+  return (size_t)m.n_kv_heads * p.n_chunks * p.rows;
+}
+size_t prefix_ws_bytes(const sf_model_cfg &m, int B, int n_q, int prefix_len, int len_upper) {
+  if (m.dtype != SF_BF16) return 0;
+  size_t own, pre = prefix_ws_rows(m, B, n_q, prefix_len, len_upper, &own);
+  return up((pre + own) * (m.head_dim + 2) * sizeof(float));
+}
+void prefix_attention(Run &r, const sf_model_cfg &m, const Prefix &pre, const void *q, const void *kc, const void *vc,
+                      const int32_t *kv_len, void *out, int B, int n_q, int cap, int mode, int len_upper,
+                      const void *qkv = nullptr, const float2 *table = nullptr, const int32_t *order = nullptr,
+                      const int32_t *slots = nullptr) {
+  if (r.st != SF_OK) return;
+  PrefixArgs p{};
+  AttnArgs &a = p.own;
+  a.q = q; a.qkv = qkv; a.table = table; a.order = order; a.slots = slots; a.kc = kc; a.vc = vc; a.kv_len = kv_len; a.out = out;
+  a.B = B; a.n_q = n_q; a.Hq = m.n_q_heads; a.Hkv = m.n_kv_heads; a.hd = m.head_dim; a.cap = cap; a.mode = mode;
+  a.part_always = 1;
+  p.pk = pre.k; p.pv = pre.v; p.len = pre.len; p.cap = pre.cap;
+  if (m.dtype != SF_BF16) { LAUNCH(K_ATTN, launch_prefix_f32(p, r.s)); return; }
+  const PrefixPlan pl = prefix_plan(B, n_q, a.Hq, a.Hkv, pre.len);
+  p.n_chunks = pl.n_chunks; p.chunk_tiles = pl.chunk_tiles; p.waves = pl.waves; p.rows = pl.rows;
+  const int n_rt = (a.Hq / a.Hkv * n_q + 31) / 32;
+  a.chunk_tiles = r.c->tune_chunk > 0 ? r.c->tune_chunk : attn_chunk_tiles(B * a.Hkv * n_rt, len_upper + n_q);
+  a.n_chunks = ((len_upper + n_q + TK - 1) / TK + a.chunk_tiles - 1) / a.chunk_tiles;
+  size_t own, rows = prefix_ws_rows(m, B, n_q, pre.len, len_upper, &own);
+  p.part_o = (float *)pre.ws; a.part_o = p.part_o + rows * a.hd;
+  p.part_ml = a.part_o + own * a.hd; a.part_ml = p.part_ml + rows * 2;
+  LAUNCH(K_ATTN, launch_prefix_bf16(p, r.s));
+  LAUNCH(K_ATTN, launch_attention_bf16(a, r.s));
+  LAUNCH(K_ATTN_COMBINE, launch_prefix_combine(p, r.s));
+}
+
 size_t kv_layer_bytes(const sf_model_cfg &m, int B, int cap) {
   return (size_t)B * m.n_kv_heads * cap * m.head_dim * esize(m.dtype);
 }
@@ -659,6 +702,35 @@ sf_status sf_op_attention(const sf_ctx *c, const void *q, const void *kc, const 
   float *part_o = (float *)workspace, *part_ml = part_o ? part_o + rows * m.head_dim : nullptr;
   Run r{c, (hipStream_t)stream};
   attention(r, m, q, kc, vc, kv_len, out, part_o, part_ml, B, n_q, cap, mask, len_upper);
+  return r.st;
+}
+
+size_t sf_prefix_attention_workspace_bytes(const sf_ctx *c, int32_t B, int32_t n_q, int32_t prefix_len, int32_t len_upper) {
+  if (!c || B < 1 || n_q < 1 || prefix_len < 0 || len_upper < 0 || (long)B * n_q > SF_PREFIX_MAX_ROWS) return 0;
+  if (prefix_len == 0) return sf_attention_workspace_bytes(c, B, n_q, len_upper);
+  return prefix_ws_bytes(c->tc, B, n_q, prefix_len, len_upper);
+}
+
+sf_status sf_op_prefix_attention(const sf_ctx *c, const void *q, const void *pk, const void *pv, int32_t prefix_len,
+                                 int32_t prefix_cap, const void *kc, const void *vc, const int32_t *kv_len, int32_t B,
+                                 int32_t n_q, int32_t cap, int32_t mask, int32_t len_upper, void *out, void *workspace,
+                                 size_t workspace_bytes, void *stream) {
+  if (!c || !q || !kc || !vc || !kv_len || !out) return SF_EINVAL;
+  if (B < 1 || n_q < 1 || cap < TK || cap % TK || len_upper < 0 || prefix_len < 0) return SF_EINVAL;
+  if (mask != SF_MASK_CAUSAL && mask != SF_MASK_BIDIR) return SF_EINVAL;
+  if (prefix_len > 0 && (!pk || !pv || prefix_cap < TK || prefix_cap % TK)) return SF_EINVAL;
+  if (((uintptr_t)q | (uintptr_t)kc | (uintptr_t)vc | (uintptr_t)out | (uintptr_t)pk | (uintptr_t)pv) % 16) return SF_EINVAL;
+  if ((long)len_upper + n_q > cap || prefix_len > prefix_cap) return SF_ECAPACITY;
+  const sf_model_cfg &m = c->tc;
+  sf_status v = check_attn_shape(m, n_q);
+  if (v != SF_OK) return v;
+  if (B > 65535 || B > SF_PREFIX_MAX_ROWS / n_q || (size_t)prefix_cap * m.head_dim * esize(m.dtype) >= (1ull << 32)) return SF_EUNSUPPORTED;
+  const size_t need = sf_prefix_attention_workspace_bytes(c, B, n_q, prefix_len, len_upper);
+  if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace) % ALIGN)) return SF_ECAPACITY;
+  if (prefix_len == 0)
+    return sf_op_attention(c, q, kc, vc, kv_len, B, n_q, cap, mask, len_upper, out, workspace, workspace_bytes, stream);
+  Run r{c, (hipStream_t)stream};
+  prefix_attention(r, m, {pk, pv, prefix_len, prefix_cap, workspace}, q, kc, vc, kv_len, out, B, n_q, cap, mask, len_upper);
   return r.st;
 }
 

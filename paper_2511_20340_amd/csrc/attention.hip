@@ -25,7 +25,8 @@ constexpr float NEG_INF = -__builtin_huge_valf();
 // rotation pair (e, e + HD/2) sits in the same lane, k-steps s and s + KS/2).  The appended rows are
 // read back by the same workgroup after a barrier; workgroups that share (sequence, kv head) own
 // disjoint tiles, or (several row groups) write identical values.
-template <int HD, int FUSE, int ONCE>
+// PART = 1: every chunk leaves a partial, the only one of a sequence too (another kernel's partials join it).
+template <int HD, int FUSE, int ONCE, int PART>
 __global__ __launch_bounds__(256, HD == 64 ? 4 : 2) void attn_bf16_kernel(
     const bf16_t *__restrict__ Q, const uint4 *Kc, const uint4 *Vc,
     const int32_t *__restrict__ kv_len, bf16_t *__restrict__ O, float *__restrict__ part_o,
@@ -43,7 +44,8 @@ __global__ __launch_bounds__(256, HD == 64 ? 4 : 2) void attn_bf16_kernel(
   const int chunk = blockIdx.x;
   const int G = Hq / Hkv;
   const int R = G * n_q;
-  const int len = min(kv_len[b], cap - n_q);  // never read past the slab, whatever the caller stored
+  // never read past the slab, whatever the caller stored
+  const int len = PART ? max(0, min(kv_len[b], cap - n_q)) : min(kv_len[b], cap - n_q);
   const int total = len + n_q;
   const int n_tiles = (total + TK - 1) / TK;
   const int t_begin = chunk * chunk_tiles;
@@ -268,7 +270,7 @@ __global__ __launch_bounds__(256, HD == 64 ? 4 : 2) void attn_bf16_kernel(
     }
   __syncthreads();
 
-  const bool direct = seq_chunks == 1;
+  const bool direct = !PART && seq_chunks == 1;
   const int rows_here = min(32, R - rt * 32);
   // 256 threads sweep the [rows_here][HD] outputs, 4 consecutive features per thread
   for (int idx = tid; idx < rows_here * (HD / 4); idx += 256) {
@@ -461,7 +463,9 @@ hipError_t launch_attention_bf16(const AttnArgs &a, hipStream_t s) {
   static bool attr_done = false;
   if (!attr_done) {
 #define SF_ATTN_LDS(HD_, FUSE_, ONCE_)                                                                    \
-  (void)hipFuncSetAttribute(reinterpret_cast<const void *>(attn_bf16_kernel<HD_, FUSE_, ONCE_>),         \
+  (void)hipFuncSetAttribute(reinterpret_cast<const void *>(attn_bf16_kernel<HD_, FUSE_, ONCE_, 0>),      \
+                            hipFuncAttributeMaxDynamicSharedMemorySize, WAVES * 32 * (HD_ + 6) * 4),     \
+  (void)hipFuncSetAttribute(reinterpret_cast<const void *>(attn_bf16_kernel<HD_, FUSE_, ONCE_, 1>),      \
                             hipFuncAttributeMaxDynamicSharedMemorySize, WAVES * 32 * (HD_ + 6) * 4)
     SF_ATTN_LDS(128, 0, 0); SF_ATTN_LDS(128, 1, 0); SF_ATTN_LDS(64, 0, 0); SF_ATTN_LDS(64, 1, 0);
     SF_ATTN_LDS(128, 0, 1); SF_ATTN_LDS(128, 1, 1); SF_ATTN_LDS(64, 0, 1); SF_ATTN_LDS(64, 1, 1);
@@ -474,18 +478,21 @@ hipError_t launch_attention_bf16(const AttnArgs &a, hipStream_t s) {
   // launch.  Several row tiles read the same keys from different workgroups: those keep the caching loads.
   // a.qkv: the raw QKV projection; the kernel rotates and appends the block's rows itself
   const bf16_t *q = (const bf16_t *)(a.qkv ? a.qkv : a.q);
-#define SF_ATTN_LAUNCH(HD_, FUSE_, ONCE_)                                                                   \
-  attn_bf16_kernel<HD_, FUSE_, ONCE_><<<grid, block, lds, s>>>(                                             \
+#define SF_ATTN_KERNEL(HD_, FUSE_, ONCE_, PART_)                                                            \
+  attn_bf16_kernel<HD_, FUSE_, ONCE_, PART_><<<grid, block, lds, s>>>(                                      \
       q, (const uint4 *)a.kc, (const uint4 *)a.vc, a.kv_len, (bf16_t *)a.out, a.part_o, a.part_ml, a.n_q,   \
       a.Hq, a.Hkv, a.cap, a.mode, a.chunk_tiles, a.n_chunks, n_rt, scale_log2e, a.table, a.order, a.slots)
+#define SF_ATTN_LAUNCH(HD_, FUSE_, ONCE_)                                                                   \
+  do { if (a.part_always) SF_ATTN_KERNEL(HD_, FUSE_, ONCE_, 1); else SF_ATTN_KERNEL(HD_, FUSE_, ONCE_, 0); } while (0)
 #define SF_ATTN_PICK(HD_)                                                                                   \
   do {                                                                                                      \
-    if (n_rt == 1) { if (a.qkv) SF_ATTN_LAUNCH(HD_, 1, 1); else SF_ATTN_LAUNCH(HD_, 0, 1); }                \
-    else           { if (a.qkv) SF_ATTN_LAUNCH(HD_, 1, 0); else SF_ATTN_LAUNCH(HD_, 0, 0); }                \
+    if (n_rt == 1) { if (a.qkv) { SF_ATTN_LAUNCH(HD_, 1, 1); } else { SF_ATTN_LAUNCH(HD_, 0, 1); } }        \
+    else           { if (a.qkv) { SF_ATTN_LAUNCH(HD_, 1, 0); } else { SF_ATTN_LAUNCH(HD_, 0, 0); } }        \
   } while (0)
   if (a.hd == 128) SF_ATTN_PICK(128); else SF_ATTN_PICK(64);
 #undef SF_ATTN_PICK
 #undef SF_ATTN_LAUNCH
+#undef SF_ATTN_KERNEL
   return hipGetLastError();
 }
 

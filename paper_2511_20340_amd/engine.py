@@ -285,6 +285,28 @@ class Engine:
         self._keep_ws = ws
         return out
 
+    def sf_op_prefix_attention(self, q, pk, pv, prefix_len, kc, vc, kv_len, n_q, mask, len_upper=None):
+        """q [B,n_q,Hq,hd]; pk/pv: tiled slabs of one sequence (layer_cache of an engine of batch 1) whose first prefix_len keys
+        every sequence continues; kc/vc/kv_len: the sequences' own keys, as sf_op_attention.  -> [B,n_q,Hq,hd]"""
+        what = "sf_op_prefix_attention"
+        B, row = q.shape[0], self.Hkv * self.hd
+        self._need(what, "q", q, (B, n_q, self.Hq, self.hd), self.tdtype)
+        self._need(what, "kv_len", kv_len, (B,), torch.int32)
+        for name, t, least in (("pk", pk, 0), ("pv", pv, 0), ("kc", kc, B * row * self.cap), ("vc", vc, B * row * self.cap)):
+            self._need(what, name, t, t.shape, self.tdtype)
+            if t.numel() < least or (least == 0 and (t.numel() != pk.numel() or t.numel() % (32 * row))):
+                raise ValueError(f"{what}: pk, pv must be slabs of one sequence of a capacity of whole tiles, kc, vc at least B slabs")
+        if len_upper is None:
+            len_upper = int(kv_len.max().item())
+        with torch.cuda.device(self.dev):
+            need = self.lib.sf_prefix_attention_workspace_bytes(self.ctx, B, n_q, prefix_len, len_upper)
+            ws, p = self._workspace(need)
+            out = torch.empty_like(q)
+            sfb.check(self.lib.sf_op_prefix_attention(self.ctx, _ptr(q), _ptr(pk), _ptr(pv), prefix_len, pk.numel() // row,
+                                                      _ptr(kc), _ptr(vc), _ptr(kv_len), B, n_q, self.cap, mask, len_upper,
+                                                      _ptr(out), p, need, _stream()), what, self.ctx)
+        return out
+
     def linear_workspace(self, M):
         """(pointer, bytes) of a split-K workspace, cached per engine."""
         nb = self.lib.sf_linear_workspace_bytes(self.ctx, M)

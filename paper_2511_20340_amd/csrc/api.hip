@@ -968,6 +968,7 @@ AcceptPlan accept_plan(int B, int k, int V) {
   p.part = take((size_t)B * segs * sizeof(double));
   p.tokens = take(rows * sizeof(int32_t));
   p.accept = take((size_t)B * sizeof(int32_t));
+  p.sample = take(rows * segs * SAMPLE_CELL_BYTES);
   p.total = off;
   return p;
 }
@@ -990,7 +991,7 @@ sf_status check_accept_sampled(int B, int k, int V, const AcceptSampled &s) {
   if (k > 0 && s.draft_logits && ((uintptr_t)s.draft_dist) % alignof(SampleDist)) return SF_EINVAL;
   if (((uintptr_t)s.workspace) % ALIGN) return SF_EINVAL;
   const long rows = (long)B * (k + 1), segs = ((long)V + SAMPLE_SEG - 1) / SAMPLE_SEG;
-  if (V > SAMPLE_MAX_VOCAB || rows > SAMPLE_MAX_ROWS || B * segs > INT32_MAX) return SF_EUNSUPPORTED;
+  if (V > SAMPLE_MAX_VOCAB || rows > SAMPLE_MAX_ROWS || rows * segs > INT32_MAX) return SF_EUNSUPPORTED;
   return s.workspace_bytes < accept_plan(B, k, V).total ? SF_ECAPACITY : SF_OK;
 }
 
@@ -1003,7 +1004,7 @@ void accept_sampled(Run &r, int B, int k, int V, const AcceptSampled &s, int32_t
   const sf_sampling &par = s.par ? *s.par : none;
   SampleDist *dist = (SampleDist *)(ws + p.dist);
   SampleArgs a{s.target_logits, B * (k + 1), V, k + 1, par.temperature, par.top_k, par.top_p, par.min_p,
-               nullptr, nullptr, nullptr, dist};
+               nullptr, nullptr, nullptr, dist, ws + p.sample, (V + SAMPLE_SEG - 1) / SAMPLE_SEG};
   LAUNCH(K_ARGMAX, launch_sample(a, r.s));
   SampleAcceptArgs c{s.draft, s.target_logits, dist, k > 0 ? s.draft_logits : nullptr, (const SampleDist *)s.draft_dist,
                      s.u_accept, s.u_sample, (double *)(ws + p.part), (int32_t *)(ws + p.tokens),
@@ -1018,8 +1019,7 @@ void accept_sampled(Run &r, int B, int k, int V, const AcceptSampled &s, int32_t
 size_t sf_sample_dist_bytes(int32_t M) { return M < 1 ? 0 : (size_t)M * sizeof(SampleDist); }
 
 size_t sf_sample_workspace_bytes(int32_t M, int32_t V) {
-  (void)M; (void)V;
-  return 0;
+  return M < 1 || V < 1 ? 0 : up((size_t)M * (((size_t)V + SAMPLE_SEG - 1) / SAMPLE_SEG) * SAMPLE_CELL_BYTES);
 }
 
 sf_status sf_op_sample(const sf_ctx *c, const float *logits, int32_t M, int32_t V, int32_t group, const sf_sampling *par,
@@ -1027,12 +1027,14 @@ sf_status sf_op_sample(const sf_ctx *c, const float *logits, int32_t M, int32_t 
                        void *stream) {
   if (!c || !logits || !u || !ids || M < 1 || V < 1 || group < 1) return SF_EINVAL;
   if (((uintptr_t)dist) % alignof(SampleDist)) return SF_EINVAL;
-  if (V > SAMPLE_MAX_VOCAB || M > SAMPLE_MAX_ROWS) return SF_EUNSUPPORTED;
+  const int segs = (V + SAMPLE_SEG - 1) / SAMPLE_SEG;
+  if (V > SAMPLE_MAX_VOCAB || M > SAMPLE_MAX_ROWS || (long)M * segs > INT32_MAX) return SF_EUNSUPPORTED;
   const size_t need = sf_sample_workspace_bytes(M, V);
   if (need && (!workspace || workspace_bytes < need || ((uintptr_t)workspace) % ALIGN)) return SF_ECAPACITY;
   const sf_sampling none{};
   if (!par) par = &none;
-  SampleArgs a{logits, M, V, group, par->temperature, par->top_k, par->top_p, par->min_p, u, ids, prob, (SampleDist *)dist};
+  SampleArgs a{logits, M, V, group, par->temperature, par->top_k, par->top_p, par->min_p, u, ids, prob, (SampleDist *)dist,
+               (char *)workspace, segs};
   Run r{c, (hipStream_t)stream};
   LAUNCH(K_ARGMAX, launch_sample(a, r.s));
   return r.st;

@@ -967,7 +967,7 @@ AcceptPlan accept_plan(int B, int k, int V) {
   p.dist = take(rows * sizeof(SampleDist));
   p.part = take((size_t)B * segs * sizeof(double));
   p.tokens = take(rows * sizeof(int32_t));
-  p.accept = take((size_t)B * sizeof(int32_t));
+  p.accept = take((size_t)2 * B * sizeof(int32_t));  // and the accepted slots
   p.sample = take(rows * segs * SAMPLE_CELL_BYTES);
   p.total = off;
   return p;
@@ -1008,7 +1008,7 @@ void accept_sampled(Run &r, int B, int k, int V, const AcceptSampled &s, int32_t
   LAUNCH(K_ARGMAX, launch_sample(a, r.s));
   SampleAcceptArgs c{s.draft, s.target_logits, dist, k > 0 ? s.draft_logits : nullptr, (const SampleDist *)s.draft_dist,
                      s.u_accept, s.u_sample, (double *)(ws + p.part), (int32_t *)(ws + p.tokens),
-                     (int32_t *)(ws + p.accept), B, k, V};
+                     (int32_t *)(ws + p.accept), (int32_t *)(ws + p.accept) + B, B, k, V};
   LAUNCH(K_ACCEPT, launch_sample_accept(c, r.s));
   AcceptArgs e{c.tokens, nullptr, c.accept, accept_len, out_tokens, kv_len, pending, n_new, cu_new, B, k};
   LAUNCH(K_ACCEPT, launch_accept(e, r.s));

@@ -26,6 +26,7 @@ namespace {
 
 constexpr int BUCKETS = 1024;    // of one refinement of the ranking
 constexpr int LIST = 2048;       // elements that are ranked by sorting
+constexpr int DIRECT = 256;      // ... without a refinement in front
 constexpr int STEP = 256;        // elements per partial sum of the draw: four to a lane of a wave
 constexpr int SEG = SAMPLE_SEG, MAX_SEGS = SAMPLE_MAX_VOCAB / SEG;
 constexpr int BINS = SAMPLE_BINS, ROOM = SAMPLE_ROOM;
@@ -56,23 +57,22 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs &a, int row) {
   return s;
 }
 
-// 2^y for y <= 0 (or a little above), to about 2^-50: the power series of 2^f, |f| <= 1/2, to the twelfth term.  The device
-// library's exp takes twice as many instructions, and double precision is a third of what these kernels do.
+// 2^y for y <= 0 (or a little above), to 2^-50: (2^f - 1) / f on |f| <= 1/2 as a polynomial of degree nine through its values at
+// the Chebyshev points.  The device library's exp takes twice as many instructions, and double precision is a third of what
+// these kernels do.
 __device__ __forceinline__ double power_of_two(double y) {
   y = fmax(y, -1200.0);  // 0 from there on, for -inf too
   const double n = rint(y), f = y - n;
-  double p = 2.5678435993488196e-11;
-  p = fma(p, f, 4.4455382718708101e-10);
-  p = fma(p, f, 7.0549116208011209e-09);
-  p = fma(p, f, 1.0178086009239696e-07);
-  p = fma(p, f, 1.3215486790144305e-06);
-  p = fma(p, f, 1.5252733804059838e-05);
-  p = fma(p, f, 1.5403530393381606e-04);
-  p = fma(p, f, 1.3333558146428441e-03);
-  p = fma(p, f, 9.6181291076284769e-03);
-  p = fma(p, f, 5.5504108664821576e-02);
-  p = fma(p, f, 2.4022650695910069e-01);
-  p = fma(p, f, 6.9314718055994529e-01);
+  double p = 7.07097786650813908e-09;
+  p = fma(p, f, 1.02059054137655955e-07);
+  p = fma(p, f, 1.32154516332214336e-06);
+  p = fma(p, f, 1.52526729248507372e-05);
+  p = fma(p, f, 1.54035304247765285e-04);
+  p = fma(p, f, 1.33335582007945925e-03);
+  p = fma(p, f, 9.61812910761866528e-03);
+  p = fma(p, f, 5.55041086646516704e-02);
+  p = fma(p, f, 2.40226506959100750e-01);
+  p = fma(p, f, 6.93147180559946174e-01);
   p = fma(p, f, 1.0);
   return __builtin_ldexp(p, (int)n);
 }
@@ -84,12 +84,48 @@ __device__ __forceinline__ double weight(float l, float top, double scale) {
   return l == top ? 1.0 : power_of_two(((double)l - (double)top) * scale);
 }
 
-// The grid of a row's buckets: bucket b holds the logits of [b, b + 1) / g.  Nucleus: eight to a factor of e in weight.
-// Counts: as wide at T >= 1/2, not narrower below, so that the tokens of a count are within reach at any temperature.
-__device__ __forceinline__ double grid_of(const Settings &s) { return 8.0 / (double)(s.kind == NUCLEUS ? s.t : fmaxf(s.t, 0.5f)); }
-constexpr double GRID_END = 1 << 20;  // beyond, a place on the grid is too coarse for the weights: the row goes without it
-__device__ __forceinline__ int bucket_of(float l, double g) {
-  return (int)floor(fmin(fmax((double)l * g, -2.0 * GRID_END), 2.0 * GRID_END));
+// The grid of a row's buckets: bucket b holds the logits of about [b, b + 1) / g (a product in float, which never puts a
+// smaller logit into a higher bucket).  Nucleus: eight to a factor of e in weight.  Counts: likewise between T = 1/2 and 2, not
+// narrower below nor wider above, so that the tokens of a count are within reach at any temperature.
+__device__ __forceinline__ double grid_of(const Settings &s) {
+  return 8.0 / (double)(s.kind == NUCLEUS ? s.t : fminf(fmaxf(s.t, 0.5f), 2.f));
+}
+constexpr float GRID_END = 1 << 16;  // beyond, a float's place on the grid is too coarse: the row goes without it
+__device__ __forceinline__ float grid_place(float l, float g) { return floorf(fmaxf(l * g, -2.f * GRID_END)); }
+__device__ __forceinline__ int bucket_of(float l, float g) { return (int)fminf(grid_place(l, g), 2.f * GRID_END); }
+
+__device__ __forceinline__ uint32_t float_order(float l) {
+  const uint32_t b = __float_as_uint(l);
+  return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float order_float(uint32_t b) { return __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b); }
+
+// The smallest float of a rising condition, from a guess that is mostly a few floats off.  It holds for hi, not for -inf.
+template <class F> __device__ __forceinline__ float first_float(float guess, float hi, F holds) {
+  uint32_t a = float_order(-INF), b = float_order(hi);
+  const uint32_t g = min(max(float_order(guess), a + 1), b);
+  if (holds(order_float(g))) {
+    b = g;
+    for (int i = 0; i < 4 && b - a > 1; ++i)
+      if (holds(order_float(b - 1))) --b; else a = b - 1;
+  } else {
+    a = g;
+    for (int i = 0; i < 4 && b - a > 1; ++i)
+      if (holds(order_float(a + 1))) b = a + 1; else ++a;
+  }
+  while (b - a > 1) {
+    const uint32_t mid = a + (b - a) / 2;
+    if (holds(order_float(mid))) b = mid; else a = mid;
+  }
+  return order_float(b);
+}
+// the first float of bucket b, b at most that of hi
+__device__ __forceinline__ float bucket_start(int b, double g, float hi) {
+  return first_float((float)((double)b / g), hi, [&](float l) { return bucket_of(l, (float)g) >= b; });
+}
+// the smallest float whose weight reaches m in (0, 1]
+__device__ __forceinline__ float least_of(float m, float t, float top, double scale) {
+  return first_float((float)((double)top + (double)t * log((double)m)), top, [&](float l) { return weight(l, top, scale) >= (double)m; });
 }
 
 // what the running weight has to exceed, within [0, z) whatever u is (NaN: the upper border)
@@ -137,17 +173,15 @@ template <int BS, class T> __device__ __forceinline__ T block_before(T v, T *red
 
 // key of the ranking: rises with the logit, among equal ones with falling index
 __device__ __forceinline__ uint64_t rank_key(float l, int i) {
-  uint32_t b = __float_as_uint(l + 0.f);  // -0 ranks as 0
-  b = b & 0x80000000u ? ~b : b | 0x80000000u;
+  const uint32_t b = float_order(l + 0.f);  // -0 ranks as 0
   return (uint64_t)b << 32 | (uint32_t)(INT_MAX - i);
 }
 __device__ __forceinline__ float key_logit(uint64_t k) {
-  const uint32_t b = (uint32_t)(k >> 32);
-  return __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b);
+  return order_float((uint32_t)(k >> 32));
 }
 __device__ __forceinline__ int key_index(uint64_t k) { return INT_MAX - (int)(uint32_t)k; }
 
-// the elements that a selection looks at, by rising index
+// the elements that a selection looks at
 struct Source {
   const float *l;
   const int32_t *idx;  // null: an element's place
@@ -162,25 +196,38 @@ struct Shared {
   uint64_t list[LIST];
   double seg[MAX_SEGS], step[SEG / STEP];  // kept weight of the segments, of a segment's steps
   uint64_t seg_lo[MAX_SEGS], seg_hi[MAX_SEGS];
-  int32_t seg_n[MAX_SEGS], seg_at[MAX_SEGS];
+  int32_t seg_n[MAX_SEGS], seg_at[MAX_SEGS], seg_task[MAX_SEGS];
   double redd[16];
   int redi[16];
   uint32_t redu[16];
-  int n_list;
+  double factor[BINS];  // of the row's bins
+  int n_list, n_mem;
   int at, found;
   double before, sum;
   int count;
 };
 
-template <int BS, class F> __device__ __forceinline__ void for_each(const Source &s, F f) {
-  for (int i0 = threadIdx.x * 4; i0 < s.n; i0 += BS * 4) {
-    if (i0 + 4 <= s.n) {
-      const f32x4u v = *reinterpret_cast<const f32x4u *>(s.l + i0);
+// x[i, i + 4) of n
+__device__ __forceinline__ f32x4u four(const float *x, int i, int n) {
+  if (i + 4 <= n) return *reinterpret_cast<const f32x4u *>(x + i);
+  f32x4u v;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) f(v[e], i0 + e);
-    } else {
-      for (int i = i0; i < s.n; ++i) f(s.l[i], i);
-    }
+  for (int e = 0; e < 4; ++e) v[e] = i + e < n ? x[i + e] : __builtin_nanf("");
+  return v;
+}
+
+// f(logit, place) for all but NaN.  Four requests of a thread are on their way at a time.
+template <int BS, class F> __device__ __forceinline__ void for_each(const Source &s, F f) {
+  constexpr int AHEAD = 4;
+  for (int i0 = threadIdx.x * 4; i0 < s.n; i0 += BS * 4 * AHEAD) {
+    f32x4u v[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) v[j] = four(s.l, i0 + j * BS * 4, s.n);
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (v[j][e] == v[j][e]) f(v[j][e], i0 + j * BS * 4 + e);
   }
 }
 
@@ -235,13 +282,13 @@ template <int BS> __device__ int nth_equal(Shared &sh, const Source &s, float v,
 // Cuts the ranking of the elements that are kept so far (l > thr or l == thr and index <= last): by_mass, behind the last
 // element in front of which less than `target` of weight lies (share >= 0: that share of the weight of these and `rest`, what
 // else there is); else behind the k best.  mass0: weight of elements that rank in front of all of these and are not among them.  thr and last receive the last
-// kept element; returns the kept weight.  lo_hint: nothing of interest is expected below; hi: nothing lies above.
+// kept element; returns the kept weight.  ties: where the j-th of equal elements is looked up (s may be in any order).  lo_hint: nothing of interest is expected below; hi: nothing lies above.
 //
 // A refinement sorts the elements of an interval of logits into buckets by a linear map (it never puts a smaller logit in
 // front of a larger one), finds the bucket of the cut from the running counts and weights, and goes on with that bucket's
 // interval, until it has few elements, which are sorted, or equal ones, which are counted.
 template <int BS>
-__device__ double cut(Shared &sh, const Source &s, bool by_mass, int k, double share, double target, double mass0, double rest,
+__device__ double cut(Shared &sh, const Source &s, const Source &ties, bool by_mass, int k, double share, double target, double mass0, double rest,
                       float top, double scale, float lo_hint, float hi, float &thr, int &last) {
   constexpr int PER = BUCKETS / BS > 0 ? BUCKETS / BS : 1;
   const int tid = threadIdx.x;
@@ -251,7 +298,7 @@ __device__ double cut(Shared &sh, const Source &s, bool by_mass, int k, double s
   float lo = fmaxf(lo_hint, thr0);            // the interval [lo, hi]; what lies above is kept whole
   bool below = true;                          // elements below lo belong to the last bucket
   int count0 = mass0 > 0.0 ? 1 : 0;           // by weight only whether there is one in front matters
-  bool whole = s.n <= LIST;                   // few elements: sorted as they are
+  const bool whole = s.n <= DIRECT;           // few elements: sorted as they are
   for (;;) {
     const double places = hi > lo ? (BUCKETS - 2) / ((double)hi - (double)lo) : 0.0;
     auto bucket = [&](float l) {
@@ -361,7 +408,7 @@ __device__ double cut(Shared &sh, const Source &s, bool by_mass, int k, double s
       if (!by_mass) j = min(n_at, k - count0);
       else if (w1 > 0.0) j = (int)fmin((double)n_at, fmax(1.0, ceil((target - mass0) / w1)));
       thr = mn;
-      last = j == n_at && mn > thr0 ? INT_MAX : nth_equal<BS>(sh, s, mn, j - 1);
+      last = j == n_at && mn > thr0 ? INT_MAX : nth_equal<BS>(sh, ties, mn, j - 1);
       return mass0 + w1 * j;
     }
     // -inf apart from the rest: elements below lo
@@ -377,34 +424,15 @@ __device__ double cut(Shared &sh, const Source &s, bool by_mass, int k, double s
   }
 }
 
-// The smallest float whose weight reaches m in (0, 1].
-__device__ float least_of(float m, float top, double scale) {
-  auto order = [](float l) { const uint32_t b = __float_as_uint(l); return b & 0x80000000u ? ~b : b | 0x80000000u; };
-  auto value = [](uint32_t b) { return __uint_as_float(b & 0x80000000u ? b & 0x7fffffffu : ~b); };
-  uint32_t lo = order(-INF), hi = order(top);  // the weight of lo is below m, that of hi is not
-  while (hi - lo > 1) {
-    const uint32_t mid = lo + (hi - lo) / 2;
-    if (weight(value(mid), top, scale) >= (double)m) hi = mid; else lo = mid;
-  }
-  return value(hi);
-}
-
-// Appends the elements (l, i) of a tile that are wanted to the row's list, by rising index: every thread passes its N
-// consecutive ones.  count: entries so far (the same in all threads); beyond `room` nothing is written.
-template <int BS, int N>
-__device__ __forceinline__ void append(Shared &sh, const float (&l)[N], const int (&i)[N], const bool (&want)[N], float *to_l,
-                                       int32_t *to_i, int room, int &count) {
-  int own = 0, all;
-#pragma unroll
-  for (int e = 0; e < N; ++e) own += want[e];
-  int at = count + block_before<BS>(own, sh.redi, all);
-#pragma unroll
-  for (int e = 0; e < N; ++e)
-    if (want[e]) {
-      if (at < room) { to_l[at] = l[e]; to_i[at] = i[e]; }
-      ++at;
-    }
-  count += all;
+// Appends the wanted elements of a wave to the row's selection, in any order between waves.
+__device__ __forceinline__ void collect(Shared &sh, bool want, float l, int i, float *to_l, int32_t *to_i, int room) {
+  const uint64_t m = __ballot(want);
+  if (m == 0) return;
+  const int lane = threadIdx.x & 63;
+  int at = 0;
+  if (lane == 0) at = atomicAdd(&sh.n_mem, __popcll(m));
+  at = __shfl(at, 0) + __popcll(m & ((1ull << lane) - 1));
+  if (want && at < room) { to_l[at] = l; to_i[at] = i; }
 }
 
 struct SegStat {
@@ -423,6 +451,9 @@ __device__ __forceinline__ size_t cells(const SampleArgs &a) { return (size_t)a.
 __device__ __forceinline__ uint64_t *bins(const SampleArgs &a) { return reinterpret_cast<uint64_t *>(a.ws + cells(a) * SAMPLE_STAT_BYTES); }
 __device__ __forceinline__ float *list_l(const SampleArgs &a) { return reinterpret_cast<float *>(bins(a) + cells(a) * BINS); }
 __device__ __forceinline__ int32_t *list_i(const SampleArgs &a) { return reinterpret_cast<int32_t *>(list_l(a) + cells(a) * ROOM); }
+// the row's selection of them, segs * ROOM a row
+__device__ __forceinline__ float *mem_l(const SampleArgs &a) { return reinterpret_cast<float *>(list_i(a) + cells(a) * ROOM); }
+__device__ __forceinline__ int32_t *mem_i(const SampleArgs &a) { return reinterpret_cast<int32_t *>(mem_l(a) + cells(a) * ROOM); }
 
 // A bin: count in the upper 14 bits, below it the sum of 2^36 exp((l - edge) / T), edge the bucket's upper end.
 constexpr int BIN_COUNT = 50;
@@ -442,15 +473,9 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
   float l[N][4];
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const int i = (j * 256 + tid) * 4;
-    if (i + 4 <= n) {
-      const f32x4u v = __builtin_nontemporal_load(reinterpret_cast<const f32x4u *>(x + i));
+    const f32x4u v = four(x, (j * 256 + tid) * 4, n);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) l[j][e] = v[e];
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) l[j][e] = i + e < n ? x[i + e] : __builtin_nanf("");
-    }
+    for (int e = 0; e < 4; ++e) l[j][e] = v[e];
   }
   const Settings st = settings_of(a, row);
   float best = -INF;
@@ -482,43 +507,57 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
     out.z = block_reduce<256>(sum, redd, [](double p, double q) { return p + q; });
   } else {
     const double g = grid_of(st);
-    out.off = !(fabs((double)top * g) < GRID_END);
+    const float gf = (float)g;
+    out.off = !(fabsf(top * gf) < GRID_END);
     if (!out.off) {
-      out.bucket = bucket_of(top, g);
+      out.bucket = bucket_of(top, gf);
       for (int b = lane; b < BINS; b += 64) hist[wave][b] = 0;  // a wave's own: no barrier
       const bool mass = st.kind == NUCLEUS;
-      const double last_edge = (double)(out.bucket - BINS + 2);
+      const float first = (float)out.bucket;
+      int limit = BINS;  // bins from there on have not counted all
+      if (mass) {
+        const double last_edge = (double)(out.bucket - BINS + 2);
 #pragma unroll
-      for (int j = 0; j < N; ++j)
+        for (int j = 0; j < N; ++j)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float v = l[j][e];
-          if (!(v > -INF)) continue;
-          const double t = (double)v * g, fl = floor(fmax(t, -2.0 * GRID_END));
-          const int rel = min(out.bucket - (int)fl, BINS - 1);
-          uint64_t add = 1ull << BIN_COUNT;
-          if (mass) {
+          for (int e = 0; e < 4; ++e) {
+            const float v = l[j][e];
+            if (!(v > -INF)) continue;
+            const float fl = grid_place(v, gf);
+            const int rel = (int)fminf(first - fl, (float)(BINS - 1));
             double w;
             if (rel < BINS - 1) {
-              // exp(f / 8), f in [-1, 0): the power series to the ninth term
-              const double f = t - (fl + 1.0);
-              w = 2.0531802791346530e-14;
-              w = fma(w, f, 1.4782898009769500e-12);
-              w = fma(w, f, 9.4610547262524802e-11);
-              w = fma(w, f, 5.2981906467013891e-09);
-              w = fma(w, f, 2.5431315104166666e-07);
-              w = fma(w, f, 1.0172526041666666e-05);
-              w = fma(w, f, 3.2552083333333332e-04);
-              w = fma(w, f, 7.8125e-03);
-              w = fma(w, f, 0.125);
-              w = fma(w, f, 1.0);
+              // exp(f / 8), f in [-1, 0] (the float product's roundings beside), as a polynomial of degree six in f + 1/2
+              // through its values at the Chebyshev points: to 2^-45, the bin takes 2^-37
+              const double f = fma((double)v, g, -0.5 - (double)fl);
+              w = 4.97784668590196699e-09;
+              w = fma(w, f, 2.38947156470155655e-07);
+              w = fma(w, f, 9.55620375649920453e-06);
+              w = fma(w, f, 3.05798517364579050e-04);
+              w = fma(w, f, 7.33916455323328255e-03);
+              w = fma(w, f, 1.17426632851876683e-01);
+              w = fma(w, f, 9.39413062813475808e-01);
             } else {
-              w = power_of_two((t - last_edge) * (LOG2E / 8.0));
+              w = power_of_two(((double)v * g - last_edge) * (LOG2E / 8.0));
             }
-            add += __builtin_bit_cast(uint64_t, fma(w, 0x1p36, 0x1p52)) & ((1ull << 52) - 1);
+            const uint64_t add = (1ull << BIN_COUNT) + (__builtin_bit_cast(uint64_t, fma(w, 0x1p36, 0x1p52)) & ((1ull << 52) - 1));
+            atomicAdd((unsigned long long *)&hist[wave][rel], (unsigned long long)add);
           }
-          atomicAdd((unsigned long long *)&hist[wave][rel], (unsigned long long)add);
-        }
+      } else {
+        // only what may get into the list is counted: nothing below the least of the threads' largest, of which there are 256
+        float bound = block_reduce<256>(best, redf, [](float p, float q) { return fminf(p, q); });
+        if (st.k != INT_MAX && st.k > 256) bound = -INF;
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float v = l[j][e];
+            if (!(v > -INF) || v < bound) continue;
+            const int rel = (int)fminf(first - grid_place(v, gf), (float)(BINS - 1));
+            atomicAdd((unsigned long long *)&hist[wave][rel], 1ull << BIN_COUNT);
+          }
+        if (bound > -INF) limit = out.bucket - bucket_of(bound, gf);
+      }
       __syncthreads();
       static_assert(BINS == 256, "a bin for each thread");
       const uint64_t bin = hist[0][tid] + hist[1][tid] + hist[2][tid] + hist[3][tid];
@@ -528,7 +567,7 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
       // with a share, until what lies below is a quarter of what the share leaves out.
       int total;
       const int cnt = (int)(bin >> BIN_COUNT), upto = cnt + block_before<256>(cnt, redi, total);
-      bool take = upto <= ROOM;
+      bool take = upto <= ROOM && tid < limit;
       if (st.k != INT_MAX) take = take && upto - cnt < st.k;
       if (st.m > 0.f && !(st.k != INT_MAX && st.p < 1.f))
         take = take && (double)(out.bucket - tid + 1) >= ((double)top + (double)st.t * log((double)st.m)) * g - 1.0;
@@ -540,17 +579,16 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
       }
       const int deep = block_reduce<256>(take ? BINS : tid, redi, [](int p, int q) { return min(p, q); });
       // the last bin also holds what lies below it: a list that takes it holds everything
-      const int cut = deep == 0 ? INT_MAX : deep >= BINS ? INT_MIN : out.bucket - deep + 1;
-      out.cut = cut;
-      if (cut != INT_MAX) {
-        auto want = [&](float v) { return v > -INF && bucket_of(v, g) >= cut; };
+      out.cut = deep == 0 ? INT_MAX : deep >= BINS ? INT_MIN : out.bucket - deep + 1;
+      if (deep > 0) {
+        const float from = deep >= BINS ? -FLT_MAX : bucket_start(out.cut, g, top);
         uint32_t flags = 0;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
           int c = 0;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const bool w = want(l[j][e]);
+            const bool w = l[j][e] >= from;
             flags |= (uint32_t)w << (j * 4 + e);
             c += __popcll(__ballot(w));
           }
@@ -585,18 +623,43 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
   if (tid == 0) stats(a)[cell] = out;
 }
 
+// over the lanes of a wave
+template <class T, class F> __device__ __forceinline__ T wave_reduce(T v, F f) {
+#pragma unroll
+  for (int o = 32; o; o >>= 1) v = f(v, __shfl_xor(v, o));
+  return v;
+}
+template <class T> __device__ __forceinline__ T wave_before(T v) {  // sum over the lanes below
+  T x = v;
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const T y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
+  x = __shfl_up(x, 1);
+  return lane == 0 ? T(0) : x;
+}
+
 // One workgroup per row.
 template <int BS>
-__global__ __launch_bounds__(BS) void row_kernel(const SampleArgs a) {
+__global__ __launch_bounds__(BS, BS == 256 ? 3 : 4) void row_kernel(const SampleArgs a) {
   __shared__ Shared sh;
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, segs = a.segs;
   const float *x = a.logits + (size_t)row * a.V;
   const SegStat *stat = stats(a) + (size_t)row * segs;
   const Settings st = settings_of(a, row);
-  SegStat mine{-INF, INT_MAX, 0, INT_MIN, 0, 0, 0.0};
-  if (tid < segs) mine = stat[tid];
-  const float top = block_reduce<BS>(mine.top, (float *)sh.redu, [](float p, float q) { return fmaxf(p, q); });
-  const int arg = block_reduce<BS>(mine.top == top ? mine.arg : INT_MAX, sh.redi, [](int p, int q) { return min(p, q); });
+  // every wave has all the segments, two to a lane
+  static_assert(MAX_SEGS == 128, "two segments to a lane");
+  SegStat own[2];
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    own[e] = SegStat{-INF, INT_MAX, 0, INT_MIN, 0, 0, 0.0};
+    if (lane + e * 64 < segs) own[e] = stat[lane + e * 64];
+  }
+  const float top = wave_reduce(fmaxf(own[0].top, own[1].top), [](float p, float q) { return fmaxf(p, q); });
+  const int arg = wave_reduce(min(own[0].top == top ? own[0].arg : INT_MAX, own[1].top == top ? own[1].arg : INT_MAX),
+                              [](int p, int q) { return min(p, q); });
   const double scale = LOG2E / (double)st.t;
   SampleDist d{top, top, arg == INT_MAX ? -1 : arg, st.t, arg == INT_MAX ? 0.0 : 1.0, arg == INT_MAX ? 0 : arg, arg == INT_MAX ? 0.f : 1.f};
   if (arg != INT_MAX && st.kind != ONE && top > -INF) {
@@ -604,244 +667,279 @@ __global__ __launch_bounds__(BS) void row_kernel(const SampleArgs a) {
     int last = INT_MAX;
     const Source all{x, nullptr, a.V};
     const float hint = top - fminf(40.f * st.t, FLT_MAX);
-    const float least = st.m > 0.f ? least_of(st.m, top, scale) : -INF;
+    const float least = st.m > 0.f ? least_of(st.m, st.t, top, scale) : -INF;
     const double g = grid_of(st);
-    float *mem_l = list_l(a) + (size_t)row * segs * ROOM;
-    int32_t *mem_i = list_i(a) + (size_t)row * segs * ROOM;
+    const float gf = (float)g;
+    const size_t cell0 = (size_t)row * segs * ROOM;
+    float *ml = mem_l(a) + cell0;
+    int32_t *mi = mem_i(a) + cell0;
     const int room = segs * ROOM;
-    // a segment that weighs nothing beside the row's largest, to the last bit, is left out
-    const bool absent = tid >= segs || mine.arg == INT_MAX || weight(mine.top, top, scale) == 0.0;
-    const float lowest = block_reduce<BS>(tid < segs && absent ? mine.top : -INF, (float *)sh.redu, [](float p, float q) { return fmaxf(p, q); });
-    // the deepest bucket from which on every segment's list is whole
-    const int whole = block_reduce<BS>(!absent ? mine.cut : INT_MIN, sh.redi, [](int p, int q) { return max(p, q); });
-    const bool off = block_reduce<BS>(!absent && mine.off ? 1 : 0, sh.redi, [](int p, int q) { return p | q; });
-    // joins the segments' lists from bucket `from` up to bucket `upto`, by rising index, in the place of the first
-    auto join = [&](int from, int upto) {
-      int n = 0;
-      if (tid < segs) sh.seg_n[tid] = absent ? 0 : mine.n;
-      __syncthreads();
-      for (int s = 0; s < segs; ++s) {
-        const int ns = sh.seg_n[s];
-        for (int i0 = 0; i0 < ns; i0 += BS) {
-          const int i = i0 + tid;
-          float l[1] = {0.f};
-          int idx[1] = {0};
-          bool want[1] = {false};
-          if (i < ns) {
-            l[0] = mem_l[s * ROOM + i];
-            idx[0] = mem_i[s * ROOM + i];
-            const int b = bucket_of(l[0], g);
-            want[0] = b >= from && b <= upto;
+    int whole = INT_MIN, off = 0;  // the deepest bucket from which on every segment's list is whole; off the grid
+    float lowest = -INF;           // the largest of the segments that are left out
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      // a segment that weighs nothing beside the row's largest, to the last bit, is left out
+      if (own[e].arg == INT_MAX || weight(own[e].top, top, scale) == 0.0) {
+        lowest = fmaxf(lowest, own[e].top);
+        own[e].arg = INT_MAX;
+      } else {
+        whole = max(whole, own[e].cut);
+        off |= own[e].off;
+      }
+    }
+    whole = wave_reduce(whole, [](int p, int q) { return max(p, q); });
+    off = wave_reduce(off, [](int p, int q) { return p | q; });
+    lowest = wave_reduce(lowest, [](float p, float q) { return fmaxf(p, q); });
+    // the lists in pieces of 64 entries: the pieces of the segments up to each lane's
+    int n0 = own[0].arg != INT_MAX ? (own[0].n + 63) / 64 : 0, n1 = own[1].arg != INT_MAX ? (own[1].n + 63) / 64 : 0;
+    const int all0 = wave_reduce(n0, [](int p, int q) { return p + q; });
+    const int end0 = wave_before(n0) + n0, end1 = all0 + wave_before(n1) + n1;
+    const int pieces = all0 + wave_reduce(n1, [](int p, int q) { return p + q; });
+    if (wave == 0) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int s = lane + e * 64;
+        const bool there = own[e].arg != INT_MAX;
+        sh.seg_n[s] = there ? own[e].n : 0;
+        sh.seg_at[s] = there ? own[e].bucket : INT_MIN;
+        sh.seg_task[s] = e ? end1 - n1 : end0 - n0;
+        sh.seg_lo[s] = 0; sh.seg_hi[s] = 0;
+        sh.seg[s] = there && st.kind == ALL ? own[e].z * weight(own[e].top, top, scale) : 0.0;
+      }
+      if (lane == 0) sh.n_mem = 0;
+    }
+    __syncthreads();
+    // selects what lies in [from, to) of the segments' lists
+    auto join = [&](float from, float to) {
+      constexpr int AHEAD = 4;
+      for (int t0 = wave; t0 < pieces; t0 += BS / 64 * AHEAD) {
+        float l[AHEAD];
+        int i[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+          const int t = t0 + j * (BS / 64);
+          l[j] = __builtin_nanf(""); i[j] = 0;
+          if (t < pieces) {
+            // the segment: the first whose pieces end behind t
+            const int s = __popcll(__ballot(end0 <= t)) + __popcll(__ballot(end1 <= t));
+            const int at = (t - sh.seg_task[s]) * 64 + lane;
+            if (at < sh.seg_n[s]) {
+              l[j] = list_l(a)[cell0 + s * ROOM + at];
+              i[j] = list_i(a)[cell0 + s * ROOM + at];
+            }
           }
-          append<BS>(sh, l, idx, want, mem_l, mem_i, room, n);  // its barrier stands between these reads and its writes
         }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) collect(sh, l[j] >= from && l[j] < to, l[j], i[j], ml, mi, room);
       }
       __syncthreads();
-      return n;
+      return min(sh.n_mem, room);
     };
-    // kept weight of the segments from the elements of a source, exact whatever the order
+    // kept weight of the segments from the selection, exact whatever the order
     auto add_kept = [&](const Source &s) {
       for_each<BS>(s, [&](float l, int i) {
-        const int idx = s.idx ? s.idx[i] : i;
+        const int idx = s.idx[i];
         if (!(l > thr || (l == thr && idx <= last))) return;
         const uint64_t fx = (uint64_t)(weight(l, top, scale) * 0x1p62);
         atomicAdd((unsigned long long *)&sh.seg_lo[idx / SEG], (unsigned long long)(fx & 0xffffffffu));
         atomicAdd((unsigned long long *)&sh.seg_hi[idx / SEG], (unsigned long long)(fx >> 32));
       });
-      __syncthreads();
     };
-    for (int s = tid; s < segs; s += BS) { sh.seg_lo[s] = 0; sh.seg_hi[s] = 0; sh.seg[s] = 0.0; }
-    __syncthreads();
-    bool done = false;
-    if (st.kind == ALL) {
-      if (tid < segs) sh.seg[tid] = mine.arg == INT_MAX ? 0.0 : mine.z * weight(mine.top, top, scale);
-      __syncthreads();
-      done = true;
-    } else if (st.kind == NUCLEUS && !off) {
-      // the row's histogram, from the bucket of its largest downward; a segment's starts at its own largest
-      const int first = bucket_of(top, g);
-      if (tid < segs) sh.seg_at[tid] = absent ? INT_MIN : mine.bucket;
-      __syncthreads();
-      const uint64_t *h = bins(a) + (size_t)row * segs * BINS;
-      // thread b < BINS - 1 has the row's bucket first - b; all that lies deeper is summed by segment
-      double here = 0.0;
-      int cnt = 0;
-      if (tid < BINS - 1) {
-        uint64_t m = 0;
-        for (int s = 0; s < segs; ++s) {
-          const int fs = sh.seg_at[s], rel = tid - (first - fs);
-          if (fs == INT_MIN || rel < 0) continue;  // deeper than BINS - 1 it cannot be: fs <= first
-          const uint64_t bin = h[(size_t)s * BINS + rel];
-          m += bin & BIN_MASS;
-          cnt += (int)(bin >> BIN_COUNT);
+    // the same from the logits
+    auto add_row = [&]() {
+      for (int s = wave; s < segs; s += BS / 64) {
+        const int n = min(a.V - s * SEG, SEG);
+        double sum = 0.0;
+        for (int i0 = lane * 4; i0 < n; i0 += STEP * 4) {
+          f32x4u v[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) v[j] = four(x + s * SEG, i0 + j * STEP, n);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (v[j][e] > thr || (v[j][e] == thr && s * SEG + i0 + j * STEP + e <= last)) sum += weight(v[j][e], top, scale);
         }
-        here = (double)m * 0x1p-36 * power_of_two(((double)(first - tid + 1) - (double)top * g) * (LOG2E / 8.0));
+        sum = wave_reduce(sum, [](double p, double q) { return p + q; });
+        if (lane == 0) sh.seg[s] = sum;
       }
+    };
+    bool done = st.kind == ALL;
+    if (st.kind == NUCLEUS && !off) {
+      // The row's histogram, from the bucket of its largest downward (a segment's starts at its own largest), and what lies
+      // deeper.  Whole numbers until they are weighed.
+      const int first = bucket_of(top, gf);
+      const uint64_t *h = bins(a) + (size_t)row * segs * BINS;
+      const double edge = (double)top * g;
+      for (int b = tid; b < BINS; b += BS) {
+        sh.h.lo[b] = 0;
+        sh.h.cnt[b] = 0;
+        sh.factor[b] = power_of_two(((double)(first - b + 1) - edge) * (LOG2E / 8.0)) * 0x1p-36;
+      }
+      __syncthreads();
       double deep = 0.0;
-      for (int c = tid; c < segs * BINS; c += BS) {
-        const int s = c / BINS, rel = c % BINS, fs = sh.seg_at[s];
-        if (fs == INT_MIN || rel + (first - fs) < BINS - 1) continue;
-        deep += (double)(h[c] & BIN_MASS) * 0x1p-36 * power_of_two(((double)(fs - rel + 1) - (double)top * g) * (LOG2E / 8.0));
+      constexpr int AHEAD = 4;
+      for (int c0 = tid; c0 < segs * BINS; c0 += BS * AHEAD) {
+        uint64_t v[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+          const int c = c0 + j * BS;
+          v[j] = c < segs * BINS && sh.seg_at[c / BINS] != INT_MIN ? h[c] : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+          if (v[j] == 0) continue;
+          const int c = c0 + j * BS, rel = c % BINS + (first - sh.seg_at[c / BINS]);
+          if (c % BINS < BINS - 1 && rel < BINS - 1) {
+            atomicAdd((unsigned long long *)&sh.h.lo[rel], (unsigned long long)(v[j] & BIN_MASS));
+            atomicAdd(&sh.h.cnt[rel], (uint32_t)(v[j] >> BIN_COUNT));
+          } else {
+            deep += (double)(v[j] & BIN_MASS) * power_of_two(((double)(first - rel + 1) - edge) * (LOG2E / 8.0));
+          }
+        }
       }
-      deep = block_reduce<BS>(deep, sh.redd, [](double p, double q) { return p + q; });
+      deep = block_reduce<BS>(deep, sh.redd, [](double p, double q) { return p + q; }) * 0x1p-36;
+      const int cnt = tid < BINS - 1 ? (int)sh.h.cnt[tid] : 0;
+      const double here = tid < BINS - 1 ? (double)sh.h.lo[tid] * sh.factor[tid] : 0.0;
       double z;
       const double before = block_before<BS>(here, sh.redd, z);
       const double target = (double)st.p * (z + deep);
-      int ctot;
-      const int cbefore = block_before<BS>(cnt, sh.redi, ctot);
-      const int at = block_reduce<BS>(cnt > 0 && (before < target || cbefore == 0) ? tid : -1, sh.redi, [](int p, int q) { return max(p, q); });
-      // target lies in what is deeper: the histogram does not tell where
-      const bool reach = z >= target && at >= 0;
+      const int at = block_reduce<BS>(cnt > 0 && (before < target || tid == 0) ? tid : -1, sh.redi, [](int p, int q) { return max(p, q); });
       if (at == tid) { sh.before = before; sh.count = cnt; sh.sum = z - here; }
       __syncthreads();
-      if (reach) {
-        const int b = first - at, n_b = sh.count;
-        const double mass0 = sh.before, rest = sh.sum + deep;
-        Source mem{mem_l, mem_i, 0};
-        bool have = true;
+      const int b = first - at, n_b = sh.count;
+      const double mass0 = sh.before, rest = sh.sum + deep;
+      // Where the target lies in what is deeper, the histogram does not tell; a bucket of too many is left to the row.
+      if (z >= target && at >= 0 && (b >= whole || n_b <= room)) {
+        const float lo_b = bucket_start(b, g, top), hi_b = b == first ? INF : bucket_start(b + 1, g, top);
+        Source mem{ml, mi, 0};
         if (b >= whole) {
-          mem.n = join(b, b);
-        } else if (n_b <= room) {
+          mem.n = join(lo_b, hi_b);
+        } else {
           // not in the lists: from the logits
-          int n = 0;
-          for (int i0 = 0; i0 < a.V; i0 += BS * 4) {
-            float l[4];
-            int idx[4];
-            bool want[4];
-            const int i = i0 + tid * 4;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              l[e] = i + e < a.V ? x[i + e] : -INF;
-              idx[e] = i + e;
-              want[e] = l[e] > -INF && bucket_of(l[e], g) == b;
+          for_each<BS>(all, [&](float l, int i) {
+            if (l >= lo_b && l < hi_b) {
+              const int place = atomicAdd(&sh.n_mem, 1);
+              if (place < room) { ml[place] = l; mi[place] = i; }
             }
-            append<BS>(sh, l, idx, want, mem_l, mem_i, room, n);
-          }
+          });
           __syncthreads();
-          mem.n = n;
-        } else {
-          have = false;
+          mem.n = min(sh.n_mem, room);
         }
-        if (have) {
-          // the bucket's ends, a little wider
-          const float lo_b = (float)((b - 0.01) / g), hi_b = fminf(top, (float)((b + 1.01) / g));
-          // The bucket's weight anew from its elements: histogram and weights differ in the last bits, and among equal
-          // logits the border may fall on an element exactly.
-          (void)cut<BS>(sh, mem, true, 0, (double)st.p, 0.0, mass0, rest, top, scale, lo_b, hi_b, thr, last);
-          if (least > thr) { thr = least; last = INT_MAX; }
-          if (bucket_of(thr, g) == b) {
-            // of every segment: the buckets above, and what is kept of this one
-            for (int s = wave; s < segs; s += BS / 64) {
-              const int fs = sh.seg_at[s];
-              double sum = 0.0;
-              if (fs != INT_MIN)
-                for (int rel = lane; rel < min(BINS - 1, fs - b); rel += 64)
-                  sum += (double)(h[(size_t)s * BINS + rel] & BIN_MASS) * 0x1p-36 *
-                         power_of_two(((double)(fs - rel + 1) - (double)top * g) * (LOG2E / 8.0));
+        // The bucket's weight anew from its elements: histogram and weights differ in the last bits, and among equal
+        // logits the border may fall on an element exactly.
+        (void)cut<BS>(sh, mem, all, true, 0, (double)st.p, 0.0, mass0, rest, top, scale, lo_b, fminf(top, hi_b), thr, last);
+        if (least > thr) { thr = least; last = INT_MAX; }
+        if (thr < hi_b) {
+          // of every segment: the buckets above, and what is kept of this one
+          for (int c0 = wave * 64; c0 < segs * BINS; c0 += BS * 2) {
+            uint64_t v[2];
 #pragma unroll
-              for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-              if (lane == 0) sh.seg[s] = sum;
+            for (int j = 0; j < 2; ++j) {
+              const int c = c0 + j * BS + lane, fs = sh.seg_at[min(c / BINS, segs - 1)];
+              v[j] = c < segs * BINS && fs != INT_MIN && fs - c % BINS > b ? h[c] & BIN_MASS : 0;
             }
-            __syncthreads();
-            add_kept(mem);
-            done = true;
-          }  // else the least weight cuts higher: below, over the row
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              if (!__any(v[j] != 0)) continue;
+              const int c = c0 + j * BS + lane, s = c / BINS;
+              // in multiples of 2^-49: a segment's tokens weigh less than 2^14 together
+              const uint64_t fx = v[j] ? (uint64_t)((double)v[j] * sh.factor[first - sh.seg_at[s] + c % BINS] * 0x1p49) : 0;
+              const uint64_t sum = wave_reduce(fx, [](uint64_t p, uint64_t q) { return p + q; });
+              if (lane == 0) {
+                atomicAdd((unsigned long long *)&sh.seg_lo[s], (unsigned long long)((sum << 13) & 0xffffffffu));
+                atomicAdd((unsigned long long *)&sh.seg_hi[s], (unsigned long long)(sum >> 19));
+              }
+            }
+          }
+          add_kept(mem);
         } else {
-          thr = -INF;
+          add_row();  // the least weight cuts higher
         }
-        if (!done && have) { add_kept(all); done = true; }
+        done = true;
       }
-    } else if (st.kind == FEW && !off) {
-      if (whole != INT_MAX) {
-        const int n = join(whole, INT_MAX);
-        const Source mem{mem_l, mem_i, n};
-        if (n >= st.k) {
-          const double w = cut<BS>(sh, mem, false, st.k, -1.0, 0.0, 0.0, 0.0, top, scale, hint, top, thr, last);
-          if (st.p < 1.f) (void)cut<BS>(sh, mem, true, 0, -1.0, (double)st.p * w, 0.0, 0.0, top, scale, hint, top, thr, last);
-          done = thr > lowest;  // else a segment without a list may have one of them
-          if (least > thr) { thr = least; last = INT_MAX; }
-        } else if ((st.k == INT_MAX || st.p >= 1.f) && (whole == INT_MIN || bucket_of(least, g) >= whole) && st.m > 0.f) {
-          thr = least;
-          done = true;
-        }
-        if (done) add_kept(mem);
+    } else if (st.kind == FEW && !off && whole != INT_MAX) {
+      const int n = join(whole == INT_MIN ? -INF : bucket_start(whole, g, top), INF);
+      const Source mem{ml, mi, n};
+      if (n >= st.k) {
+        const double w = cut<BS>(sh, mem, all, false, st.k, -1.0, 0.0, 0.0, 0.0, top, scale, hint, top, thr, last);
+        if (st.p < 1.f) (void)cut<BS>(sh, mem, all, true, 0, -1.0, (double)st.p * w, 0.0, 0.0, top, scale, hint, top, thr, last);
+        done = thr > lowest;  // else a segment without a list may have one of them
+        if (least > thr) { thr = least; last = INT_MAX; }
+      } else if ((st.k == INT_MAX || st.p >= 1.f) && st.m > 0.f && (whole == INT_MIN || bucket_of(least, gf) >= whole)) {
+        thr = least;
+        done = true;
       }
+      if (done) add_kept(mem);
     }
     if (!done) {
       // the whole row, refinement by refinement
       thr = -INF; last = INT_MAX;
       double w = -1.0;
-      if (st.k != INT_MAX) w = cut<BS>(sh, all, false, st.k, -1.0, 0.0, 0.0, 0.0, top, scale, hint, top, thr, last);
-      if (st.p < 1.f) (void)cut<BS>(sh, all, true, 0, w < 0.0 ? (double)st.p : -1.0, (double)st.p * w, 0.0, 0.0, top, scale, hint, top, thr, last);
+      if (st.k != INT_MAX) w = cut<BS>(sh, all, all, false, st.k, -1.0, 0.0, 0.0, 0.0, top, scale, hint, top, thr, last);
+      if (st.p < 1.f) (void)cut<BS>(sh, all, all, true, 0, w < 0.0 ? (double)st.p : -1.0, (double)st.p * w, 0.0, 0.0, top, scale, hint, top, thr, last);
       if (least > thr) { thr = least; last = INT_MAX; }
-      add_kept(all);
+      add_row();
     }
-    // kept weight in front of every segment; the segment that the target falls into
-    double own = 0.0, z;
-    if (tid < segs) own = sh.seg[tid] + from_fixed(sh.seg_lo[tid], sh.seg_hi[tid]);
-    const double before = block_before<BS>(own, sh.redd, z);
+    __syncthreads();
+    // kept weight in front of every segment; the segment that the target falls into (every wave by itself)
+    const double w0 = sh.seg[lane] + from_fixed(sh.seg_lo[lane], sh.seg_hi[lane]);
+    const double w1 = sh.seg[lane + 64] + from_fixed(sh.seg_lo[lane + 64], sh.seg_hi[lane + 64]);
+    const double z0 = wave_reduce(w0, [](double p, double q) { return p + q; });
+    const double z = z0 + wave_reduce(w1, [](double p, double q) { return p + q; });
     d.thr = thr; d.last = last; d.z = z;
     if (a.u) {
-      const double target = target_of(a.u[row], z);
-      const int seg = block_reduce<BS>(own > 0.0 && before <= target ? tid : -1, sh.redi, [](int p, int q) { return max(p, q); });
-      if (tid == seg) sh.before = before;
-      const int i0 = seg * SEG, n_steps = (min(a.V - i0, SEG) + STEP - 1) / STEP;
-      auto step_weights = [&](int s, double (&w)[4]) {
-        double sum = 0.0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int i = i0 + s * STEP + lane * 4 + e;
-          const float l = i < a.V ? x[i] : -INF;
-          w[e] = i < a.V && (l > thr || (l == thr && i <= last)) ? weight(l, top, scale) : 0.0;
-          sum += w[e];
-        }
-        return sum;
-      };
-      double w[4];
-      if (seg >= 0) {
-        for (int s = wave; s < n_steps; s += BS / 64) {
-          double sum = step_weights(s, w);
-#pragma unroll
-          for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o);
-          if (lane == 0) sh.step[s] = sum;
-        }
-      }
-      __syncthreads();
-      if (seg >= 0 && wave == 0) {
-        // the step: the last that starts at or before the target (rounding may put all behind it: the first of weight)
-        const double v = lane < n_steps ? sh.step[lane] : 0.0;
-        double incl = v;
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-          const double y = __shfl_up(incl, o);
-          if (lane >= o) incl += y;
-        }
-        const double start = sh.before + (incl - v);
-        const uint64_t some = __ballot(v > 0.0), fit = __ballot(v > 0.0 && start <= target);
-        if (some) {
-          const int s = fit ? 63 - __clzll(fit) : __ffsll((unsigned long long)some) - 1;
-          double run = __shfl(start, s);
-          const double own_w = step_weights(s, w);
-          double in = own_w;
-#pragma unroll
-          for (int o = 1; o < 64; o <<= 1) {
-            const double y = __shfl_up(in, o);
-            if (lane >= o) in += y;
-          }
-          run += in - own_w;
-          int id = -1, any = -1;
-          double wid = 0.0, wany = 0.0;
+      const double target = target_of(a.u[row], z), b0 = wave_before(w0), b1 = z0 + wave_before(w1);
+      const uint64_t in0 = __ballot(w0 > 0.0 && b0 <= target), in1 = __ballot(w1 > 0.0 && b1 <= target);
+      if (in0 | in1) {
+        const int seg = in1 ? 127 - __clzll(in1) : 63 - __clzll(in0);
+        const double seg_before = __shfl(seg < 64 ? b0 : b1, seg & 63);
+        const int n = min(a.V - seg * SEG, SEG), n_steps = (n + STEP - 1) / STEP;
+        const float *xs = x + seg * SEG;
+        auto weights = [&](const f32x4u &l, int i, double (&w)[4]) {
+          double sum = 0.0;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            run += w[e];
-            if (w[e] > 0.0) { any = i0 + s * STEP + lane * 4 + e; wany = w[e]; }
-            if (id < 0 && w[e] > 0.0 && run > target) { id = any; wid = w[e]; }
+            w[e] = 0.0;
+            if (l[e] > thr || (l[e] == thr && seg * SEG + i + e <= last)) w[e] = weight(l[e], top, scale);
+            sum += w[e];
           }
-          // the first lane that passes the target; where rounding lets none, the last token of weight
-          const uint64_t over = __ballot(id >= 0), has = __ballot(any >= 0);
-          const int lane_at = over ? __ffsll((unsigned long long)over) - 1 : 63 - __clzll(has);
-          d.id = __shfl(over ? id : any, lane_at);
-          d.prob = (float)(__shfl(over ? wid : wany, lane_at) / z);
+          return sum;
+        };
+        constexpr int PER = SEG / STEP / (BS / 64);  // steps of a wave
+        f32x4u v[PER];
+        double w[4];
+#pragma unroll
+        for (int j = 0; j < PER; ++j) v[j] = four(xs, (j * (BS / 64) + wave) * STEP + lane * 4, n);
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+          const int s = j * (BS / 64) + wave;
+          const double sum = wave_reduce(weights(v[j], s * STEP + lane * 4, w), [](double p, double q) { return p + q; });
+          if (lane == 0) sh.step[s] = sum;
+        }
+        __syncthreads();
+        if (wave == 0) {
+          // the step: the last that starts at or before the target (rounding may put all behind it: the first of weight)
+          const double sum = lane < n_steps ? sh.step[lane] : 0.0, start = seg_before + wave_before(sum);
+          const uint64_t some = __ballot(sum > 0.0), fit = __ballot(sum > 0.0 && start <= target);
+          if (some) {
+            const int s = fit ? 63 - __clzll(fit) : __ffsll((unsigned long long)some) - 1, i = s * STEP + lane * 4;
+            const double mine = weights(four(xs, i, n), i, w);
+            double run = __shfl(start, s) + wave_before(mine);
+            int id = -1, any = -1;
+            double wid = 0.0, wany = 0.0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              run += w[e];
+              if (w[e] > 0.0) { any = seg * SEG + i + e; wany = w[e]; }
+              if (id < 0 && w[e] > 0.0 && run > target) { id = any; wid = w[e]; }
+            }
+            // the first lane that passes the target; where rounding lets none, the last token of weight
+            const uint64_t over = __ballot(id >= 0), has = __ballot(any >= 0);
+            const int lane_at = over ? __ffsll((unsigned long long)over) - 1 : 63 - __clzll(has);
+            d.id = __shfl(over ? id : any, lane_at);
+            d.prob = (float)(__shfl(over ? wid : wany, lane_at) / z);
+          }
         }
       }
     }
@@ -867,10 +965,19 @@ struct Rest {
   SampleDist pd, qd;
   double p_t, p_z, q_t, q_z;
   int dead;            // token that a draft without logits is certain of (-1: none)
-  __device__ __forceinline__ double at(int i) const {
-    const double pi = share_of(pd, p_t, p_z, p[i], i);
-    if (q) return fmax(pi - share_of(qd, q_t, q_z, q[i], i), 0.0);
-    return i == dead ? 0.0 : pi;
+  // of the four tokens from i on, whose logits are lp and lq
+  __device__ __forceinline__ double at(const f32x4u &lp, const f32x4u &lq, int i, double (&r)[4]) const {
+    double sum = 0.0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      r[e] = 0.0;
+      if (kept_by(pd, lp[e], i + e) && i + e != dead) {
+        r[e] = weight(lp[e], pd.top, p_t) * p_z;
+        if (q) r[e] = fmax(r[e] - share_of(qd, q_t, q_z, lq[e], i + e), 0.0);
+      }
+      sum += r[e];
+    }
+    return sum;
   }
 };
 __device__ __forceinline__ double inv_of(double z) { return z > 0.0 ? 1.0 / z : 0.0; }
@@ -914,77 +1021,109 @@ __device__ Rest rest_of(const SampleAcceptArgs &a, int b, int n) {
   return r;
 }
 
-// One workgroup per (sequence, segment of the vocabulary): the segment's rest.
+// Four consecutive tokens of a lane in each of the segment's steps of 256; of NW waves this one's.
+template <int NW, class F> __device__ __forceinline__ void rest_steps(const Rest &r, int i0, int V, F f) {
+  constexpr int PER = SEG / STEP / NW, AHEAD = PER < 4 ? PER : 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int j0 = 0; j0 < PER; j0 += AHEAD) {
+    f32x4u p[AHEAD], q[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const int i = i0 + ((j0 + j) * NW + wave) * STEP + lane * 4;
+      p[j] = four(r.p, i, V);
+      q[j] = r.q ? four(r.q, i, V) : p[j];
+    }
+#pragma unroll
+    for (int j = 0; j < AHEAD; ++j) {
+      const int s = (j0 + j) * NW + wave;
+      double w[4];
+      f(s, r.at(p[j], q[j], i0 + s * STEP + lane * 4, w));
+    }
+  }
+}
+
+// One workgroup per (sequence, segment of the vocabulary): the segment's rest, and by the first one the accepted slots.
 __global__ __launch_bounds__(256) void rest_sum_kernel(const SampleAcceptArgs a, int segs) {
   __shared__ int redi[4];
   __shared__ double redd[4];
   const int b = blockIdx.x / segs, seg = blockIdx.x % segs;
-  const Rest r = rest_of(a, b, accepted(a, b, redi));
+  const int n = accepted(a, b, redi);
+  const Rest r = rest_of(a, b, n);
   double sum = 0.0;
-  for (int i = seg * SAMPLE_SEG + threadIdx.x; i < min(a.V, (seg + 1) * SAMPLE_SEG); i += 256) sum += r.at(i);
+  rest_steps<4>(r, seg * SEG, a.V, [&](int, double s) { sum += s; });
   sum = block_reduce<256>(sum, redd, [](double x, double y) { return x + y; });
-  if (threadIdx.x == 0) a.part[(size_t)b * segs + seg] = sum;
+  if (threadIdx.x == 0) {
+    a.part[(size_t)b * segs + seg] = sum;
+    if (seg == 0) a.n[b] = n;
+  }
 }
 
 // One workgroup per sequence: the token behind the accepted slots.
-__global__ __launch_bounds__(256) void rest_draw_kernel(const SampleAcceptArgs a, int segs) {
-  __shared__ int redi[4];
-  __shared__ double redd[4], step[SAMPLE_SEG / 64], found;
+__global__ __launch_bounds__(1024) void rest_draw_kernel(const SampleAcceptArgs a, int segs) {
+  __shared__ double part[MAX_SEGS], step[SEG / STEP];
   const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int n = accepted(a, b, redi);
+  const int n = a.n[b];
   Rest r = rest_of(a, b, n);
-  double *part = a.part + (size_t)b * segs;
-  double own = tid < segs ? part[tid] : 0.0, z, before = block_before<256>(own, redd, z);
+  if (tid < MAX_SEGS) part[tid] = tid < segs ? a.part[(size_t)b * segs + tid] : 0.0;
+  __syncthreads();
+  double w0 = part[lane], w1 = part[lane + 64];
+  auto add = [](double p, double q) { return p + q; };
+  double z0 = wave_reduce(w0, add), z = z0 + wave_reduce(w1, add);
   if (!(z > 0.0)) {
     // nothing is left (target and draft agree, and the drafted token has no share in either): the target's own
     r.q = nullptr; r.dead = -1;
-    for (int s = 0; s < segs; ++s) {
-      double sum = 0.0;
-      for (int i = s * SAMPLE_SEG + tid; i < min(a.V, (s + 1) * SAMPLE_SEG); i += 256) sum += r.at(i);
-      sum = block_reduce<256>(sum, redd, [](double x, double y) { return x + y; });
-      if (tid == s) own = sum;
-    }
-    before = block_before<256>(own, redd, z);
-  }
-  const double target = target_of(a.u_sample[b], z);
-  const int seg = block_reduce<256>(own > 0.0 && before <= target ? tid : -1, redi, [](int x, int y) { return max(x, y); });
-  int id = max(r.pd.id, 0);
-  if (seg >= 0) {
-    if (tid == seg) found = before;
-    const int i0 = seg * SAMPLE_SEG, i1 = min(a.V, i0 + SAMPLE_SEG), steps = (i1 - i0 + 63) / 64;
-    for (int s = wave; s < steps; s += 4) {
-      const int i = i0 + s * 64 + lane;
-      double v = i < i1 ? r.at(i) : 0.0;
-#pragma unroll
-      for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-      if (lane == 0) step[s] = v;
-    }
     __syncthreads();
-    const double x = tid < steps ? step[tid] : 0.0;
-    double tot;
-    const double run = found + block_before<256>(x, redd, tot);
-    const int hit = block_reduce<256>(x > 0.0 && run <= target ? tid : -1, redi, [](int p, int q) { return max(p, q); });
-    // rounding may put the segment's first token behind the target
-    const int s = hit >= 0 ? hit : block_reduce<256>(x > 0.0 ? tid : INT_MAX, redi, [](int p, int q) { return min(p, q); });
-    if (tid == s) found = run;
-    __syncthreads();
-    if (wave == 0 && s < steps) {
-      const int i = i0 + s * 64 + lane;
-      const double v = i < i1 ? r.at(i) : 0.0;
-      double incl = v;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const double y = __shfl_up(incl, o);
-        if (lane >= o) incl += y;
+    for (int s = wave; s < segs; s += 16) {
+      double sum = 0.0, w[4];
+      for (int i = s * SEG + lane * 4; i < min(a.V, (s + 1) * SEG); i += STEP) {
+        const f32x4u p = four(r.p, i, a.V);
+        sum += r.at(p, p, i, w);
       }
-      const uint64_t some = __ballot(v > 0.0), over = __ballot(v > 0.0 && found + incl > target);
-      if (some) id = i0 + s * 64 + (over ? __ffsll((unsigned long long)over) - 1 : 63 - __clzll(some));
+      sum = wave_reduce(sum, add);
+      if (lane == 0) part[s] = sum;
+    }
+    __syncthreads();
+    w0 = part[lane]; w1 = part[lane + 64];
+    z0 = wave_reduce(w0, add); z = z0 + wave_reduce(w1, add);
+  }
+  const double target = target_of(a.u_sample[b], z), b0 = wave_before(w0), b1 = z0 + wave_before(w1);
+  const uint64_t in0 = __ballot(w0 > 0.0 && b0 <= target), in1 = __ballot(w1 > 0.0 && b1 <= target);
+  int id = max(r.pd.id, 0);
+  if (in0 | in1) {
+    const int seg = in1 ? 127 - __clzll(in1) : 63 - __clzll(in0), i0 = seg * SEG;
+    const double seg_before = __shfl(seg < 64 ? b0 : b1, seg & 63);
+    rest_steps<16>(r, i0, a.V, [&](int s, double mine) {
+      const double sum = wave_reduce(mine, add);
+      if (lane == 0) step[s] = sum;
+    });
+    __syncthreads();
+    if (wave == 0) {
+      // the step: the last that starts at or before the target (rounding may put all behind it: the first of weight)
+      const double sum = lane < SEG / STEP ? step[lane] : 0.0, start = seg_before + wave_before(sum);
+      const uint64_t some = __ballot(sum > 0.0), fit = __ballot(sum > 0.0 && start <= target);
+      if (some) {
+        const int s = fit ? 63 - __clzll(fit) : __ffsll((unsigned long long)some) - 1, i = i0 + s * STEP + lane * 4;
+        const f32x4u p = four(r.p, i, a.V);
+        double w[4];
+        const double mine = r.at(p, r.q ? four(r.q, i, a.V) : p, i, w);
+        double run = __shfl(start, s) + wave_before(mine);
+        int hit = -1, any = -1;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          run += w[e];
+          if (w[e] > 0.0) any = i + e;
+          if (hit < 0 && w[e] > 0.0 && run > target) hit = any;
+        }
+        const uint64_t over = __ballot(hit >= 0), has = __ballot(any >= 0);
+        id = __shfl(over ? hit : any, over ? __ffsll((unsigned long long)over) - 1 : 63 - __clzll(has));
+      }
     }
   }
-  if (tid <= n) a.tokens[(size_t)b * (a.k + 1) + tid] = tid < n ? a.draft[(size_t)b * a.k + tid] : -1;
-  __syncthreads();
+  int32_t *tokens = a.tokens + (size_t)b * (a.k + 1);
+  if (tid < n) tokens[tid] = a.draft[(size_t)b * a.k + tid];
   if (tid == 0) {
-    a.tokens[(size_t)b * (a.k + 1) + n] = id;
+    tokens[n] = id;
     a.accept[b] = n + 1;
   }
 }
@@ -996,7 +1135,7 @@ hipError_t launch_sample_accept(const SampleAcceptArgs &a, hipStream_t s) {
   rest_sum_kernel<<<a.B * segs, 256, 0, s>>>(a, segs);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  rest_draw_kernel<<<a.B, 256, 0, s>>>(a, segs);
+  rest_draw_kernel<<<a.B, 1024, 0, s>>>(a, segs);
   return hipGetLastError();
 }
 

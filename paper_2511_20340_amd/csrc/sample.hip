@@ -20,13 +20,13 @@
 #include "sf_internal.h"
 #include <float.h>
 #include <limits.h>
+#include <stdlib.h>
 
 namespace sf {
 namespace {
 
 constexpr int BUCKETS = 1024;    // of one refinement of the ranking
-constexpr int LIST = 2048;       // elements that are ranked by sorting
-constexpr int DIRECT = 256;      // ... without a refinement in front
+constexpr int LIST = 512;        // elements that are ranked one by one
 constexpr int STEP = 256;        // elements per partial sum of the draw: four to a lane of a wave
 constexpr int SEG = SAMPLE_SEG, MAX_SEGS = SAMPLE_MAX_VOCAB / SEG;
 constexpr int BINS = SAMPLE_BINS, ROOM = SAMPLE_ROOM;
@@ -51,7 +51,7 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs &a, int row) {
   if (s.k <= 0 || s.k >= a.V) s.k = INT_MAX;
   if (a.V == 1 || !(s.t > 0.f)) { s.t = 1.f; s.k = 1; }  // greedy
   s.t = fminf(s.t, FLT_MAX);                 // keeps 1 / t above zero: -inf times it stays -inf
-  if (!(s.p < 1.f)) s.p = 1.f;
+  s.p = s.p < 1.f ? fmaxf(s.p, 0.f) : 1.f;
   if (!(s.m > 0.f)) s.m = 0.f;
   s.kind = s.k == 1 || s.m > 1.f ? ONE : s.k != INT_MAX ? FEW : s.p < 1.f ? NUCLEUS : s.m > 0.f ? FEW : ALL;
   return s;
@@ -193,7 +193,7 @@ struct Shared {
     uint32_t cnt[BUCKETS];
     uint64_t lo[BUCKETS], hi[BUCKETS];  // weight * 2^62, its lower 32 bits and the rest
   } h;
-  uint64_t list[LIST];
+  uint64_t list[LIST], sorted[LIST];
   double seg[MAX_SEGS], step[SEG / STEP];  // kept weight of the segments, of a segment's steps
   uint64_t seg_lo[MAX_SEGS], seg_hi[MAX_SEGS];
   int32_t seg_n[MAX_SEGS], seg_at[MAX_SEGS], seg_task[MAX_SEGS];
@@ -233,21 +233,20 @@ template <int BS, class F> __device__ __forceinline__ void for_each(const Source
 
 __device__ __forceinline__ double from_fixed(uint64_t lo, uint64_t hi) { return (double)hi * 0x1p-30 + (double)lo * 0x1p-62; }
 
-// sorts sh.list[0, LIST) by falling key
+// sh.sorted = sh.list[0, n) by falling key.  An element's place is the number of larger ones: 512 elements take 1.5 us, a
+// network of exchanges with a barrier in each of its 45 steps takes ten.
 template <int BS> __device__ void sort_list(Shared &sh, int n) {
-  int m = 2;
-  while (m < n) m <<= 1;
-  for (int i = n + threadIdx.x; i < m; i += BS) sh.list[i] = 0;
+  constexpr int PARTS = BS > LIST ? BS / LIST : 1;  // lanes that share an element's comparisons
+  for (int e = threadIdx.x / PARTS; e < n; e += BS / PARTS) {
+    const uint64_t key = sh.list[e];
+    int place = 0;
+#pragma unroll 8
+    for (int j = threadIdx.x % PARTS; j < n; j += PARTS) place += sh.list[j] > key;
+#pragma unroll
+    for (int o = 1; o < PARTS; o <<= 1) place += __shfl_xor(place, o);
+    if (threadIdx.x % PARTS == 0) sh.sorted[place] = key;
+  }
   __syncthreads();
-  for (int size = 2; size <= m; size <<= 1)
-    for (int d = size >> 1; d; d >>= 1) {
-      for (int x = threadIdx.x; x < m / 2; x += BS) {
-        const int i = (x & (d - 1)) + 2 * (x & ~(d - 1)), j = i + d;
-        const uint64_t a = sh.list[i], b = sh.list[j];
-        if ((a < b) == ((i & size) == 0)) { sh.list[i] = b; sh.list[j] = a; }
-      }
-      __syncthreads();
-    }
 }
 
 // The j-th (from 0) element by index among those equal to v.
@@ -279,6 +278,41 @@ template <int BS> __device__ int nth_equal(Shared &sh, const Source &s, float v,
   return r;
 }
 
+// Of sh.list[0, n), n <= LIST: ranks them and cuts behind the k best, and of those (share < 1) behind the last in front of
+// which less than share of the weight lies: of the k best's, or, without a count, of all these and `rest`'s.  target >= 0: the
+// weight itself.  mass0: weight of elements that rank in front and are not among them.  Returns how many stay (sh.sorted) and
+// their weight, mass0 with it.
+template <int BS>
+__device__ int ranked(Shared &sh, int n, int k, double share, double target, double mass0, double rest, float top, double scale,
+                      double &kept) {
+  constexpr int EACH = LIST / BS > 0 ? LIST / BS : 1;
+  const int tid = threadIdx.x;
+  sort_list<BS>(sh, n);
+  double x[EACH], xs = 0.0, all;
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    const int i = tid * EACH + e;
+    x[e] = i < n && i < k ? weight(key_logit(sh.sorted[i]), top, scale) : 0.0;
+    xs += x[e];
+  }
+  double run = mass0 + block_before<BS>(xs, sh.redd, all);
+  if (target < 0.0) target = share < 1.0 ? share * (k == INT_MAX ? rest + all : mass0 + all) : INF;
+  int keep = -1;
+  double sum = 0.0;
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    const int i = tid * EACH + e;
+    const bool in = i < n && i < k && (run < target || (i == 0 && !(mass0 > 0.0)));
+    run += x[e];
+    if (in) { keep = i; sum = run; }
+  }
+  const int end = block_reduce<BS>(keep, sh.redi, [](int a, int b) { return max(a, b); });
+  if (keep == end && end >= 0) sh.sum = sum;
+  __syncthreads();
+  kept = end >= 0 ? sh.sum : mass0;
+  return end + 1;
+}
+
 // Cuts the ranking of the elements that are kept so far (l > thr or l == thr and index <= last): by_mass, behind the last
 // element in front of which less than `target` of weight lies (share >= 0: that share of the weight of these and `rest`, what
 // else there is); else behind the k best.  mass0: weight of elements that rank in front of all of these and are not among them.  thr and last receive the last
@@ -298,7 +332,7 @@ __device__ double cut(Shared &sh, const Source &s, const Source &ties, bool by_m
   float lo = fmaxf(lo_hint, thr0);            // the interval [lo, hi]; what lies above is kept whole
   bool below = true;                          // elements below lo belong to the last bucket
   int count0 = mass0 > 0.0 ? 1 : 0;           // by weight only whether there is one in front matters
-  const bool whole = s.n <= DIRECT;           // few elements: sorted as they are
+  const bool whole = s.n <= LIST;             // few elements: ranked as they are
   for (;;) {
     const double places = hi > lo ? (BUCKETS - 2) / ((double)hi - (double)lo) : 0.0;
     auto bucket = [&](float l) {
@@ -362,35 +396,13 @@ __device__ double cut(Shared &sh, const Source &s, const Source &ties, bool by_m
       __syncthreads();
       n_at = sh.n_list;
       if (n_at == 0) { thr = thr0; last = last0; return mass0; }
-      sort_list<BS>(sh, n_at);
-      // running weight of the sorted elements
-      constexpr int EACH = LIST / BS;
-      double x[EACH], xs = 0.0, xt;
-#pragma unroll
-      for (int e = 0; e < EACH; ++e) {
-        const int i = tid * EACH + e;
-        x[e] = i < n_at ? weight(key_logit(sh.list[i]), top, scale) : 0.0;
-        xs += x[e];
-      }
-      double run = mass0 + block_before<BS>(xs, sh.redd, xt);
-      if (share >= 0.0) target = share * (rest + xt);
-      int keep = -1;
-      double sum = 0.0;
-#pragma unroll
-      for (int e = 0; e < EACH; ++e) {
-        const int i = tid * EACH + e;
-        const bool in = by_mass ? run < target || count0 + i == 0 : count0 + i < k;
-        run += x[e];
-        if (i < n_at && in) { keep = i; sum = run; }
-      }
-      const int end = block_reduce<BS>(keep, sh.redi, [](int a, int b) { return max(a, b); });
-      if (keep == end && end >= 0) sh.sum = sum;
-      __syncthreads();
-      double r = mass0;
-      if (end >= 0) {
-        thr = key_logit(sh.list[end]);
-        last = key_index(sh.list[end]);
-        r = sh.sum;
+      if (share >= 0.0) target = -1.0;
+      double r;
+      const int n_kept = ranked<BS>(sh, n_at, by_mass ? INT_MAX : k - count0, by_mass && share >= 0.0 ? share : 1.0,
+                                    by_mass ? target : -1.0, mass0, rest, top, scale, r);
+      if (n_kept > 0) {
+        thr = key_logit(sh.sorted[n_kept - 1]);
+        last = key_index(sh.sorted[n_kept - 1]);
       }
       __syncthreads();
       return r;
@@ -424,15 +436,31 @@ __device__ double cut(Shared &sh, const Source &s, const Source &ties, bool by_m
   }
 }
 
-// Appends the wanted elements of a wave to the row's selection, in any order between waves.
-__device__ __forceinline__ void collect(Shared &sh, bool want, float l, int i, float *to_l, int32_t *to_i, int room) {
-  const uint64_t m = __ballot(want);
-  if (m == 0) return;
+// Appends N elements of each lane of a wave, where wanted, to the row's selection, in any order; the first to sh.list as well.
+template <int N>
+__device__ __forceinline__ void collect(Shared &sh, const bool (&want)[N], const float (&l)[N], const int (&i)[N], float *to_l,
+                                        int32_t *to_i, int room) {
+  int c = 0;
+#pragma unroll
+  for (int e = 0; e < N; ++e) c += want[e];
+  if (!__any(c != 0)) return;
   const int lane = threadIdx.x & 63;
+  int x = c;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int y = __shfl_up(x, o);
+    if (lane >= o) x += y;
+  }
   int at = 0;
-  if (lane == 0) at = atomicAdd(&sh.n_mem, __popcll(m));
-  at = __shfl(at, 0) + __popcll(m & ((1ull << lane) - 1));
-  if (want && at < room) { to_l[at] = l; to_i[at] = i; }
+  if (lane == 63) at = atomicAdd(&sh.n_mem, x);
+  at = __shfl(at, 63) + x - c;
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (want[e]) {
+      if (at < room) { to_l[at] = l[e]; to_i[at] = i[e]; }
+      if (at < LIST) sh.list[at] = rank_key(l[e], i[e]);
+      ++at;
+    }
 }
 
 struct SegStat {
@@ -643,7 +671,7 @@ template <class T> __device__ __forceinline__ T wave_before(T v) {  // sum over 
 
 // One workgroup per row.
 template <int BS>
-__global__ __launch_bounds__(BS, BS == 256 ? 3 : 4) void row_kernel(const SampleArgs a) {
+__global__ __launch_bounds__(BS, BS == 256 ? 3 : BS == 512 ? 2 : 4) void row_kernel(const SampleArgs a) {
   __shared__ Shared sh;
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, segs = a.segs;
   const float *x = a.logits + (size_t)row * a.V;
@@ -662,7 +690,9 @@ __global__ __launch_bounds__(BS, BS == 256 ? 3 : 4) void row_kernel(const Sample
                               [](int p, int q) { return min(p, q); });
   const double scale = LOG2E / (double)st.t;
   SampleDist d{top, top, arg == INT_MAX ? -1 : arg, st.t, arg == INT_MAX ? 0.0 : 1.0, arg == INT_MAX ? 0 : arg, arg == INT_MAX ? 0.f : 1.f};
+  int writer = 0;  // wave that knows the token
   if (arg != INT_MAX && st.kind != ONE && top > -INF) {
+    const float u = a.u ? a.u[row] : 0.f;
     float thr = -INF;
     int last = INT_MAX;
     const Source all{x, nullptr, a.V};
@@ -729,21 +759,39 @@ __global__ __launch_bounds__(BS, BS == 256 ? 3 : 4) void row_kernel(const Sample
             }
           }
         }
+        bool want[AHEAD];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) collect(sh, l[j] >= from && l[j] < to, l[j], i[j], ml, mi, room);
+        for (int j = 0; j < AHEAD; ++j) want[j] = l[j] >= from && l[j] < to;
+        collect(sh, want, l, i, ml, mi, room);
       }
       __syncthreads();
       return min(sh.n_mem, room);
     };
     // kept weight of the segments from the selection, exact whatever the order
+    auto add_one = [&](float l, int idx) {
+      const uint64_t fx = (uint64_t)(weight(l, top, scale) * 0x1p62);
+      atomicAdd((unsigned long long *)&sh.seg_lo[idx / SEG], (unsigned long long)(fx & 0xffffffffu));
+      atomicAdd((unsigned long long *)&sh.seg_hi[idx / SEG], (unsigned long long)(fx >> 32));
+    };
     auto add_kept = [&](const Source &s) {
       for_each<BS>(s, [&](float l, int i) {
         const int idx = s.idx[i];
-        if (!(l > thr || (l == thr && idx <= last))) return;
-        const uint64_t fx = (uint64_t)(weight(l, top, scale) * 0x1p62);
-        atomicAdd((unsigned long long *)&sh.seg_lo[idx / SEG], (unsigned long long)(fx & 0xffffffffu));
-        atomicAdd((unsigned long long *)&sh.seg_hi[idx / SEG], (unsigned long long)(fx >> 32));
+        if (l > thr || (l == thr && idx <= last)) add_one(l, idx);
       });
+    };
+    // a selection of up to LIST elements lies in sh.list: cut there (see ranked), its kept ones added
+    auto cut_list = [&](int n, int k, double mass0, double rest) {
+      double kept;
+      const int n_kept = ranked<BS>(sh, n, k, (double)st.p, -1.0, mass0, rest, top, scale, kept);
+      if (n_kept > 0) {
+        thr = key_logit(sh.sorted[n_kept - 1]);
+        last = key_index(sh.sorted[n_kept - 1]);
+      }
+      if (least > thr) { thr = least; last = INT_MAX; }
+      for (int i = tid; i < n_kept; i += BS) {
+        const float l = key_logit(sh.sorted[i]);
+        if (l >= thr) add_one(l, key_index(sh.sorted[i]));
+      }
     };
     // the same from the logits
     auto add_row = [&]() {
@@ -778,7 +826,7 @@ __global__ __launch_bounds__(BS, BS == 256 ? 3 : 4) void row_kernel(const Sample
       }
       __syncthreads();
       double deep = 0.0;
-      constexpr int AHEAD = 4;
+      constexpr int AHEAD = 8;
       for (int c0 = tid; c0 < segs * BINS; c0 += BS * AHEAD) {
         uint64_t v[AHEAD];
 #pragma unroll
@@ -817,30 +865,47 @@ __global__ __launch_bounds__(BS, BS == 256 ? 3 : 4) void row_kernel(const Sample
           mem.n = join(lo_b, hi_b);
         } else {
           // not in the lists: from the logits
-          for_each<BS>(all, [&](float l, int i) {
-            if (l >= lo_b && l < hi_b) {
-              const int place = atomicAdd(&sh.n_mem, 1);
-              if (place < room) { ml[place] = l; mi[place] = i; }
+          constexpr int N = 4;
+          for (int i0 = 0; i0 < a.V; i0 += BS * 4 * N) {
+            float l[4 * N];
+            int idx[4 * N];
+            bool want[4 * N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+              const int i = i0 + (j * BS + tid) * 4;
+              const f32x4u v = four(x, i, a.V);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                l[j * 4 + e] = v[e];
+                idx[j * 4 + e] = i + e;
+                want[j * 4 + e] = v[e] >= lo_b && v[e] < hi_b;
+              }
             }
-          });
+            collect(sh, want, l, idx, ml, mi, room);
+          }
           __syncthreads();
           mem.n = min(sh.n_mem, room);
         }
         // The bucket's weight anew from its elements: histogram and weights differ in the last bits, and among equal
         // logits the border may fall on an element exactly.
-        (void)cut<BS>(sh, mem, all, true, 0, (double)st.p, 0.0, mass0, rest, top, scale, lo_b, fminf(top, hi_b), thr, last);
-        if (least > thr) { thr = least; last = INT_MAX; }
+        if (mem.n <= LIST) {
+          cut_list(mem.n, INT_MAX, mass0, rest);
+        } else {
+          (void)cut<BS>(sh, mem, all, true, 0, (double)st.p, 0.0, mass0, rest, top, scale, lo_b, fminf(top, hi_b), thr, last);
+          if (least > thr) { thr = least; last = INT_MAX; }
+          if (thr < hi_b) add_kept(mem);
+        }
         if (thr < hi_b) {
           // of every segment: the buckets above, and what is kept of this one
-          for (int c0 = wave * 64; c0 < segs * BINS; c0 += BS * 2) {
-            uint64_t v[2];
+          for (int c0 = wave * 64; c0 < segs * BINS; c0 += BS * AHEAD) {
+            uint64_t v[AHEAD];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int j = 0; j < AHEAD; ++j) {
               const int c = c0 + j * BS + lane, fs = sh.seg_at[min(c / BINS, segs - 1)];
               v[j] = c < segs * BINS && fs != INT_MIN && fs - c % BINS > b ? h[c] & BIN_MASS : 0;
             }
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int j = 0; j < AHEAD; ++j) {
               if (!__any(v[j] != 0)) continue;
               const int c = c0 + j * BS + lane, s = c / BINS;
               // in multiples of 2^-49: a segment's tokens weigh less than 2^14 together
@@ -852,7 +917,6 @@ __global__ __launch_bounds__(BS, BS == 256 ? 3 : 4) void row_kernel(const Sample
               }
             }
           }
-          add_kept(mem);
         } else {
           add_row();  // the least weight cuts higher
         }
@@ -861,19 +925,25 @@ __global__ __launch_bounds__(BS, BS == 256 ? 3 : 4) void row_kernel(const Sample
     } else if (st.kind == FEW && !off && whole != INT_MAX) {
       const int n = join(whole == INT_MIN ? -INF : bucket_start(whole, g, top), INF);
       const Source mem{ml, mi, n};
-      if (n >= st.k) {
+      const bool in_list = n <= LIST && n >= st.k;
+      if (in_list) {
+        cut_list(n, st.k, 0.0, 0.0);
+        done = thr > lowest;  // else a segment without a list may have one of them
+      } else if (n >= st.k) {
         const double w = cut<BS>(sh, mem, all, false, st.k, -1.0, 0.0, 0.0, 0.0, top, scale, hint, top, thr, last);
         if (st.p < 1.f) (void)cut<BS>(sh, mem, all, true, 0, -1.0, (double)st.p * w, 0.0, 0.0, top, scale, hint, top, thr, last);
-        done = thr > lowest;  // else a segment without a list may have one of them
+        done = thr > lowest;
         if (least > thr) { thr = least; last = INT_MAX; }
       } else if ((st.k == INT_MAX || st.p >= 1.f) && st.m > 0.f && (whole == INT_MIN || bucket_of(least, gf) >= whole)) {
         thr = least;
         done = true;
       }
-      if (done) add_kept(mem);
+      if (done && !in_list) add_kept(mem);
     }
     if (!done) {
       // the whole row, refinement by refinement
+      __syncthreads();
+      for (int s = tid; s < segs; s += BS) { sh.seg_lo[s] = 0; sh.seg_hi[s] = 0; }
       thr = -INF; last = INT_MAX;
       double w = -1.0;
       if (st.k != INT_MAX) w = cut<BS>(sh, all, all, false, st.k, -1.0, 0.0, 0.0, 0.0, top, scale, hint, top, thr, last);
@@ -889,7 +959,7 @@ __global__ __launch_bounds__(BS, BS == 256 ? 3 : 4) void row_kernel(const Sample
     const double z = z0 + wave_reduce(w1, [](double p, double q) { return p + q; });
     d.thr = thr; d.last = last; d.z = z;
     if (a.u) {
-      const double target = target_of(a.u[row], z), b0 = wave_before(w0), b1 = z0 + wave_before(w1);
+      const double target = target_of(u, z), b0 = wave_before(w0), b1 = z0 + wave_before(w1);
       const uint64_t in0 = __ballot(w0 > 0.0 && b0 <= target), in1 = __ballot(w1 > 0.0 && b1 <= target);
       if (in0 | in1) {
         const int seg = in1 ? 127 - __clzll(in1) : 63 - __clzll(in0);
@@ -918,13 +988,18 @@ __global__ __launch_bounds__(BS, BS == 256 ? 3 : 4) void row_kernel(const Sample
           if (lane == 0) sh.step[s] = sum;
         }
         __syncthreads();
-        if (wave == 0) {
-          // the step: the last that starts at or before the target (rounding may put all behind it: the first of weight)
-          const double sum = lane < n_steps ? sh.step[lane] : 0.0, start = seg_before + wave_before(sum);
-          const uint64_t some = __ballot(sum > 0.0), fit = __ballot(sum > 0.0 && start <= target);
-          if (some) {
-            const int s = fit ? 63 - __clzll(fit) : __ffsll((unsigned long long)some) - 1, i = s * STEP + lane * 4;
-            const double mine = weights(four(xs, i, n), i, w);
+        // the step: the last that starts at or before the target (rounding may put all behind it: the first of weight)
+        const double sum = lane < n_steps ? sh.step[lane] : 0.0, start = seg_before + wave_before(sum);
+        const uint64_t some = __ballot(sum > 0.0), fit = __ballot(sum > 0.0 && start <= target);
+        if (some) {
+          const int s = fit ? 63 - __clzll(fit) : __ffsll((unsigned long long)some) - 1, i = s * STEP + lane * 4;
+          writer = s % (BS / 64);
+          if (wave == writer) {  // it has the step's logits
+            f32x4u l = v[0];
+#pragma unroll
+            for (int j = 1; j < PER; ++j)
+              if (s == j * (BS / 64) + wave) l = v[j];
+            const double mine = weights(l, i, w);
             double run = __shfl(start, s) + wave_before(mine);
             int id = -1, any = -1;
             double wid = 0.0, wany = 0.0;
@@ -944,7 +1019,7 @@ __global__ __launch_bounds__(BS, BS == 256 ? 3 : 4) void row_kernel(const Sample
       }
     }
   }
-  if (tid == 0) {
+  if (wave == writer && lane == 0) {
     if (a.ids) a.ids[row] = d.id;
     if (a.prob) a.prob[row] = d.prob;
     if (a.dist) a.dist[row] = d;
@@ -1143,7 +1218,9 @@ hipError_t launch_sample(const SampleArgs &a, hipStream_t s) {
   segment_kernel<<<a.M * a.segs, 256, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.M <= 256) row_kernel<1024><<<a.M, 1024, 0, s>>>(a);
+  static const int BSX = getenv("SBS") ? atoi(getenv("SBS")) : 0;
+  if (BSX == 1024) row_kernel<1024><<<a.M, 1024, 0, s>>>(a);
+  else if (BSX == 512) row_kernel<512><<<a.M, 512, 0, s>>>(a);
   else row_kernel<256><<<a.M, 256, 0, s>>>(a);
   return hipGetLastError();
 }

@@ -57,25 +57,39 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs &a, int row) {
   return s;
 }
 
+// Polynomials of doubles.  pinned: the coefficients once in scalar registers, where the compiler cannot see their values; one that
+// it sees it moves into two vector registers in front of every product that adds it, three instructions for one.
+template <int N> struct Poly {
+  double c[N];  // from the highest power
+  __device__ __forceinline__ double operator()(double x) const {
+    double p = c[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) p = fma(p, x, c[i]);
+    return p;
+  }
+};
+template <int N> __device__ __forceinline__ Poly<N> pinned(Poly<N> p) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) asm volatile("" : "+s"(p.c[i]));
+  return p;
+}
+
 // 2^y for y <= 0 (or a little above), to 2^-50: (2^f - 1) / f on |f| <= 1/2 as a polynomial of degree nine through its values at
 // the Chebyshev points.  The device library's exp takes twice as many instructions, and double precision is a third of what
 // these kernels do.
-__device__ __forceinline__ double power_of_two(double y) {
+#define POW2_POLY                                                                                                              \
+  Poly<11> {                                                                                                                   \
+    {7.07097786650813908e-09, 1.02059054137655955e-07, 1.32154516332214336e-06, 1.52526729248507372e-05,                     \
+     1.54035304247765285e-04, 1.33335582007945925e-03, 9.61812910761866528e-03, 5.55041086646516704e-02,                     \
+     2.40226506959100750e-01, 6.93147180559946174e-01, 1.0}                                                                    \
+  }
+__device__ __forceinline__ double power_of_two(double y, const Poly<11> &poly) {
   y = fmax(y, -1200.0);  // 0 from there on, for -inf too
-  const double n = rint(y), f = y - n;
-  double p = 7.07097786650813908e-09;
-  p = fma(p, f, 1.02059054137655955e-07);
-  p = fma(p, f, 1.32154516332214336e-06);
-  p = fma(p, f, 1.52526729248507372e-05);
-  p = fma(p, f, 1.54035304247765285e-04);
-  p = fma(p, f, 1.33335582007945925e-03);
-  p = fma(p, f, 9.61812910761866528e-03);
-  p = fma(p, f, 5.55041086646516704e-02);
-  p = fma(p, f, 2.40226506959100750e-01);
-  p = fma(p, f, 6.93147180559946174e-01);
-  p = fma(p, f, 1.0);
-  return __builtin_ldexp(p, (int)n);
+  const double n = rint(y);
+  return __builtin_ldexp(poly(y - n), (int)n);
 }
+__device__ __forceinline__ double power_of_two(double y) { return power_of_two(y, POW2_POLY); }
+__device__ __noinline__ double power_of_two_apart(double y) { return power_of_two(y); }  // where it is rare and the code long
 
 constexpr double LOG2E = 1.4426950408889634;
 
@@ -527,11 +541,15 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
   if (arg == INT_MAX || st.kind == ONE) {
     // nothing more
   } else if (st.kind == ALL) {
+    const Poly<11> poly = pinned(POW2_POLY);
     double sum = 0.0;
 #pragma unroll
     for (int j = 0; j < N; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum += l[j][e] == l[j][e] ? weight(l[j][e], top, scale) : 0.0;
+      for (int e = 0; e < 4; ++e) {
+        const double y = l[j][e] == top ? 0.0 : ((double)l[j][e] - (double)top) * scale;  // 2^0 is 1, NaN weighs nothing
+        sum += power_of_two(y, poly);
+      }
     out.z = block_reduce<256>(sum, redd, [](double p, double q) { return p + q; });
   } else {
     const double g = grid_of(st);
@@ -544,33 +562,37 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
       const float first = (float)out.bucket;
       int limit = BINS;  // bins from there on have not counted all
       if (mass) {
-        const double last_edge = (double)(out.bucket - BINS + 2);
+        // exp(f / 8), f in [-1, 0] (the float product's roundings beside), as a polynomial of degree six in f + 1/2 through its
+        // values at the Chebyshev points: to 2^-45, the bin takes 2^-37
+        const Poly<7> poly = pinned(Poly<7>{{4.97784668590196699e-09, 2.38947156470155655e-07, 9.55620375649920453e-06,
+                                             3.05798517364579050e-04, 7.33916455323328255e-03, 1.17426632851876683e-01,
+                                             9.39413062813475808e-01}});
+        const float from = bucket_start(out.bucket - (BINS - 2), g, top);  // below it the last bin
+        float low = top;
+        auto add = [&](int rel, double w) __attribute__((always_inline)) {
+          const uint64_t v = (1ull << BIN_COUNT) + (__builtin_bit_cast(uint64_t, fma(w, 0x1p36, 0x1p52)) & ((1ull << 52) - 1));
+          atomicAdd((unsigned long long *)&hist[wave][rel], (unsigned long long)v);
+        };
 #pragma unroll
         for (int j = 0; j < N; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float v = l[j][e];
-            if (!(v > -INF)) continue;
-            const float fl = grid_place(v, gf);
-            const int rel = (int)fminf(first - fl, (float)(BINS - 1));
-            double w;
-            if (rel < BINS - 1) {
-              // exp(f / 8), f in [-1, 0] (the float product's roundings beside), as a polynomial of degree six in f + 1/2
-              // through its values at the Chebyshev points: to 2^-45, the bin takes 2^-37
-              const double f = fma((double)v, g, -0.5 - (double)fl);
-              w = 4.97784668590196699e-09;
-              w = fma(w, f, 2.38947156470155655e-07);
-              w = fma(w, f, 9.55620375649920453e-06);
-              w = fma(w, f, 3.05798517364579050e-04);
-              w = fma(w, f, 7.33916455323328255e-03);
-              w = fma(w, f, 1.17426632851876683e-01);
-              w = fma(w, f, 9.39413062813475808e-01);
-            } else {
-              w = power_of_two(((double)v * g - last_edge) * (LOG2E / 8.0));
-            }
-            const uint64_t add = (1ull << BIN_COUNT) + (__builtin_bit_cast(uint64_t, fma(w, 0x1p36, 0x1p52)) & ((1ull << 52) - 1));
-            atomicAdd((unsigned long long *)&hist[wave][rel], (unsigned long long)add);
+            const float v = l[j][e], fl = grid_place(v, gf);
+            low = fminf(low, v);
+            if (!(v >= from)) continue;
+            const double f = fma((double)v, g, -0.5 - (double)fl);
+            add((int)(first - fl), poly(f));
           }
+        if (__any(low < from)) {
+          const double last_edge = (double)(out.bucket - BINS + 2);
+#pragma unroll
+          for (int j = 0; j < N; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float v = l[j][e];
+              if (v > -INF && v < from) add(BINS - 1, power_of_two_apart(((double)v * g - last_edge) * (LOG2E / 8.0)));
+            }
+        }
       } else {
         // only what may get into the list is counted: nothing below the least of the threads' largest, of which there are 256
         float bound = block_reduce<256>(best, redf, [](float p, float q) { return fminf(p, q); });
@@ -592,7 +614,7 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
       if (mass) bins(a)[cell * BINS + tid] = bin;
       // How deep the list goes: as far as it has room; with a count, until the segment alone has so many; with a least
       // weight (where no share of a count's weight hangs on what lies below), until below it even against this segment's largest;
-      // with a share, until what lies below is a quarter of what the share leaves out.
+      // with a share, until it has 64 and what lies below is a quarter of what the share leaves out.
       int total;
       const int cnt = (int)(bin >> BIN_COUNT), upto = cnt + block_before<256>(cnt, redi, total);
       bool take = upto <= ROOM && tid < limit;
@@ -603,7 +625,7 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
         const double here = (double)(bin & BIN_MASS) * power_of_two((double)-tid * (LOG2E / 8.0));
         double z;
         const double before = block_before<256>(here, redd, z);
-        take = take && z - before > 0.25 * (1.0 - (double)st.p) * z;
+        take = take && (upto - cnt < 64 || z - before > 0.25 * (1.0 - (double)st.p) * z);
       }
       const int deep = block_reduce<256>(take ? BINS : tid, redi, [](int p, int q) { return min(p, q); });
       // the last bin also holds what lies below it: a list that takes it holds everything

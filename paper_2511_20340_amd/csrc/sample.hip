@@ -20,13 +20,13 @@
 #include "sf_internal.h"
 #include <float.h>
 #include <limits.h>
-#include <stdlib.h>
 
 namespace sf {
 namespace {
 
 constexpr int BUCKETS = 1024;    // of one refinement of the ranking
 constexpr int LIST = 512;        // elements that are ranked one by one
+constexpr int MEM = 8192;        // elements of a row that LDS has room for
 constexpr int STEP = 256;        // elements per partial sum of the draw: four to a lane of a wave
 constexpr int SEG = SAMPLE_SEG, MAX_SEGS = SAMPLE_MAX_VOCAB / SEG;
 constexpr int BINS = SAMPLE_BINS, ROOM = SAMPLE_ROOM;
@@ -195,10 +195,13 @@ __device__ __forceinline__ float key_logit(uint64_t k) {
 }
 __device__ __forceinline__ int key_index(uint64_t k) { return INT_MAX - (int)(uint32_t)k; }
 
-// the elements that a selection looks at
-struct Source {
+// the elements that a selection looks at: a row of logits, or a list of ranking keys in LDS
+struct Row {
   const float *l;
-  const int32_t *idx;  // null: an element's place
+  int n;
+};
+struct List {
+  const uint64_t *key;
   int n;
 };
 
@@ -207,7 +210,7 @@ struct Shared {
     uint32_t cnt[BUCKETS];
     uint64_t lo[BUCKETS], hi[BUCKETS];  // weight * 2^62, its lower 32 bits and the rest
   } h;
-  uint64_t list[LIST], sorted[LIST];
+  uint64_t mem[MEM], list[LIST], sorted[LIST];
   double seg[MAX_SEGS], step[SEG / STEP];  // kept weight of the segments, of a segment's steps
   uint64_t seg_lo[MAX_SEGS], seg_hi[MAX_SEGS];
   int32_t seg_n[MAX_SEGS], seg_at[MAX_SEGS], seg_task[MAX_SEGS];
@@ -230,8 +233,8 @@ __device__ __forceinline__ f32x4u four(const float *x, int i, int n) {
   return v;
 }
 
-// f(logit, place) for all but NaN.  Four requests of a thread are on their way at a time.
-template <int BS, class F> __device__ __forceinline__ void for_each(const Source &s, F f) {
+// f(logit, index) for all but NaN.  Four requests of a thread are on their way at a time.
+template <int BS, class F> __device__ __forceinline__ void for_each(const Row &s, F f) {
   constexpr int AHEAD = 4;
   for (int i0 = threadIdx.x * 4; i0 < s.n; i0 += BS * 4 * AHEAD) {
     f32x4u v[AHEAD];
@@ -244,18 +247,21 @@ template <int BS, class F> __device__ __forceinline__ void for_each(const Source
         if (v[j][e] == v[j][e]) f(v[j][e], i0 + j * BS * 4 + e);
   }
 }
+template <int BS, class F> __device__ __forceinline__ void for_each(const List &s, F f) {
+  for (int i = threadIdx.x; i < s.n; i += BS) f(key_logit(s.key[i]), key_index(s.key[i]));
+}
 
 __device__ __forceinline__ double from_fixed(uint64_t lo, uint64_t hi) { return (double)hi * 0x1p-30 + (double)lo * 0x1p-62; }
 
-// sh.sorted = sh.list[0, n) by falling key.  An element's place is the number of larger ones: 512 elements take 1.5 us, a
+// sh.sorted = list[0, n) by falling key.  An element's place is the number of larger ones: 512 elements take 1.5 us, a
 // network of exchanges with a barrier in each of its 45 steps takes ten.
-template <int BS> __device__ void sort_list(Shared &sh, int n) {
+template <int BS> __device__ void sort_list(Shared &sh, const uint64_t *list, int n) {
   constexpr int PARTS = BS > LIST ? BS / LIST : 1;  // lanes that share an element's comparisons
   for (int e = threadIdx.x / PARTS; e < n; e += BS / PARTS) {
-    const uint64_t key = sh.list[e];
+    const uint64_t key = list[e];
     int place = 0;
 #pragma unroll 8
-    for (int j = threadIdx.x % PARTS; j < n; j += PARTS) place += sh.list[j] > key;
+    for (int j = threadIdx.x % PARTS; j < n; j += PARTS) place += list[j] > key;
 #pragma unroll
     for (int o = 1; o < PARTS; o <<= 1) place += __shfl_xor(place, o);
     if (threadIdx.x % PARTS == 0) sh.sorted[place] = key;
@@ -264,7 +270,7 @@ template <int BS> __device__ void sort_list(Shared &sh, int n) {
 }
 
 // The j-th (from 0) element by index among those equal to v.
-template <int BS> __device__ int nth_equal(Shared &sh, const Source &s, float v, int j) {
+template <int BS> __device__ int nth_equal(Shared &sh, const Row &s, float v, int j) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (threadIdx.x == 0) sh.found = -1;
   __syncthreads();
@@ -283,7 +289,7 @@ template <int BS> __device__ int nth_equal(Shared &sh, const Source &s, float v,
       const bool eq = i0 + lane < hi && s.l[min(i0 + lane, hi - 1)] == v;
       const uint64_t m = __ballot(eq);
       const int here = __popcll(m & ((1ull << lane) - 1));
-      if (eq && before + here == j) sh.found = s.idx ? s.idx[i0 + lane] : i0 + lane;
+      if (eq && before + here == j) sh.found = i0 + lane;
       before += __popcll(m);
     }
   __syncthreads();
@@ -292,16 +298,16 @@ template <int BS> __device__ int nth_equal(Shared &sh, const Source &s, float v,
   return r;
 }
 
-// Of sh.list[0, n), n <= LIST: ranks them and cuts behind the k best, and of those (share < 1) behind the last in front of
+// Of list[0, n), n <= LIST: ranks them and cuts behind the k best, and of those (share < 1) behind the last in front of
 // which less than share of the weight lies: of the k best's, or, without a count, of all these and `rest`'s.  target >= 0: the
 // weight itself.  mass0: weight of elements that rank in front and are not among them.  Returns how many stay (sh.sorted) and
 // their weight, mass0 with it.
 template <int BS>
-__device__ int ranked(Shared &sh, int n, int k, double share, double target, double mass0, double rest, float top, double scale,
+__device__ int ranked(Shared &sh, const uint64_t *list, int n, int k, double share, double target, double mass0, double rest, float top, double scale,
                       double &kept) {
   constexpr int EACH = LIST / BS > 0 ? LIST / BS : 1;
   const int tid = threadIdx.x;
-  sort_list<BS>(sh, n);
+  sort_list<BS>(sh, list, n);
   double x[EACH], xs = 0.0, all;
 #pragma unroll
   for (int e = 0; e < EACH; ++e) {
@@ -335,14 +341,14 @@ __device__ int ranked(Shared &sh, int n, int k, double share, double target, dou
 // A refinement sorts the elements of an interval of logits into buckets by a linear map (it never puts a smaller logit in
 // front of a larger one), finds the bucket of the cut from the running counts and weights, and goes on with that bucket's
 // interval, until it has few elements, which are sorted, or equal ones, which are counted.
-template <int BS>
-__device__ double cut(Shared &sh, const Source &s, const Source &ties, bool by_mass, int k, double share, double target, double mass0, double rest,
+template <int BS, class Source>
+__device__ double cut(Shared &sh, const Source &s, const Row &ties, bool by_mass, int k, double share, double target, double mass0, double rest,
                       float top, double scale, float lo_hint, float hi, float &thr, int &last) {
   constexpr int PER = BUCKETS / BS > 0 ? BUCKETS / BS : 1;
   const int tid = threadIdx.x;
   const float thr0 = thr;
   const int last0 = last;
-  auto kept = [&](float l, int i) { return l > thr0 || (l == thr0 && (s.idx ? s.idx[i] : i) <= last0); };
+  auto kept = [&](float l, int i) { return l > thr0 || (l == thr0 && i <= last0); };
   float lo = fmaxf(lo_hint, thr0);            // the interval [lo, hi]; what lies above is kept whole
   bool below = true;                          // elements below lo belong to the last bucket
   int count0 = mass0 > 0.0 ? 1 : 0;           // by weight only whether there is one in front matters
@@ -405,14 +411,14 @@ __device__ double cut(Shared &sh, const Source &s, const Source &ties, bool by_m
       if (tid == 0) sh.n_list = 0;
       __syncthreads();
       for_each<BS>(s, [&](float l, int i) {
-        if (inside(l, i) && bucket(l) == at) sh.list[atomicAdd(&sh.n_list, 1)] = rank_key(l, s.idx ? s.idx[i] : i);
+        if (inside(l, i) && bucket(l) == at) sh.list[atomicAdd(&sh.n_list, 1)] = rank_key(l, i);
       });
       __syncthreads();
       n_at = sh.n_list;
       if (n_at == 0) { thr = thr0; last = last0; return mass0; }
       if (share >= 0.0) target = -1.0;
       double r;
-      const int n_kept = ranked<BS>(sh, n_at, by_mass ? INT_MAX : k - count0, by_mass && share >= 0.0 ? share : 1.0,
+      const int n_kept = ranked<BS>(sh, sh.list, n_at, by_mass ? INT_MAX : k - count0, by_mass && share >= 0.0 ? share : 1.0,
                                     by_mass ? target : -1.0, mass0, rest, top, scale, r);
       if (n_kept > 0) {
         thr = key_logit(sh.sorted[n_kept - 1]);
@@ -450,31 +456,29 @@ __device__ double cut(Shared &sh, const Source &s, const Source &ties, bool by_m
   }
 }
 
-// Appends N elements of each lane of a wave, where wanted, to the row's selection, in any order; the first to sh.list as well.
+// Appends N elements of each lane of a wave, where wanted, to sh.mem, in any order; sh.n_mem counts those that find no room too.
 template <int N>
-__device__ __forceinline__ void collect(Shared &sh, const bool (&want)[N], const float (&l)[N], const int (&i)[N], float *to_l,
-                                        int32_t *to_i, int room) {
+__device__ __forceinline__ void collect(Shared &sh, const bool (&want)[N], const float (&l)[N], const int (&i)[N]) {
+  uint64_t m[N];
   int c = 0;
 #pragma unroll
-  for (int e = 0; e < N; ++e) c += want[e];
-  if (!__any(c != 0)) return;
-  const int lane = threadIdx.x & 63;
-  int x = c;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int y = __shfl_up(x, o);
-    if (lane >= o) x += y;
+  for (int e = 0; e < N; ++e) {
+    m[e] = __ballot(want[e]);
+    c += __popcll(m[e]);
   }
+  if (c == 0) return;
+  const int lane = threadIdx.x & 63;
   int at = 0;
-  if (lane == 63) at = atomicAdd(&sh.n_mem, x);
-  at = __shfl(at, 63) + x - c;
+  if (lane == 0) at = atomicAdd(&sh.n_mem, c);
+  at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
-  for (int e = 0; e < N; ++e)
+  for (int e = 0; e < N; ++e) {
     if (want[e]) {
-      if (at < room) { to_l[at] = l[e]; to_i[at] = i[e]; }
-      if (at < LIST) sh.list[at] = rank_key(l[e], i[e]);
-      ++at;
+      const int p = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m[e], 0));
+      if (p < MEM) sh.mem[p] = rank_key(l[e], i[e]);
     }
+    at += __popcll(m[e]);
+  }
 }
 
 struct SegStat {
@@ -482,7 +486,7 @@ struct SegStat {
   int32_t arg;    // lowest index of the largest; INT_MAX: no comparable value
   int32_t bucket; // of the largest on the row's grid: the histogram's first
   int32_t cut;    // the list holds all of the segment's elements from this bucket on; INT_MAX: not even the first
-  int32_t n;      // entries of the list
+  int32_t n;      // entries of the list, in any order
   int32_t off;    // the grid does not reach the values
   double z;       // ALL: sum of weights against the segment's largest
 };
@@ -493,9 +497,6 @@ __device__ __forceinline__ size_t cells(const SampleArgs &a) { return (size_t)a.
 __device__ __forceinline__ uint64_t *bins(const SampleArgs &a) { return reinterpret_cast<uint64_t *>(a.ws + cells(a) * SAMPLE_STAT_BYTES); }
 __device__ __forceinline__ float *list_l(const SampleArgs &a) { return reinterpret_cast<float *>(bins(a) + cells(a) * BINS); }
 __device__ __forceinline__ int32_t *list_i(const SampleArgs &a) { return reinterpret_cast<int32_t *>(list_l(a) + cells(a) * ROOM); }
-// the row's selection of them, segs * ROOM a row
-__device__ __forceinline__ float *mem_l(const SampleArgs &a) { return reinterpret_cast<float *>(list_i(a) + cells(a) * ROOM); }
-__device__ __forceinline__ int32_t *mem_i(const SampleArgs &a) { return reinterpret_cast<int32_t *>(mem_l(a) + cells(a) * ROOM); }
 
 // A bin: count in the upper 14 bits, below it the sum of 2^36 exp((l - edge) / T), edge the bucket's upper end.
 constexpr int BIN_COUNT = 50;
@@ -506,7 +507,7 @@ static_assert(SEG < 1 << 14, "a bin counts a segment");
 __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
   __shared__ uint64_t hist[4][BINS];  // one a wave
   __shared__ float redf[4];
-  __shared__ int32_t redi[4], counts[SEG / 1024][4];
+  __shared__ int32_t redi[4], n_list;
   __shared__ double redd[4];
   constexpr int N = SEG / 1024;
   const int row = blockIdx.x / a.segs, seg = blockIdx.x % a.segs, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -515,7 +516,8 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
   float l[N][4];
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const f32x4u v = four(x, (j * 256 + tid) * 4, n);
+    const int i = (j * 256 + tid) * 4;
+    const f32x4u v = n == SEG ? *reinterpret_cast<const f32x4u *>(x + i) : four(x, i, n);
 #pragma unroll
     for (int e = 0; e < 4; ++e) l[j][e] = v[e];
   }
@@ -541,15 +543,19 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
   if (arg == INT_MAX || st.kind == ONE) {
     // nothing more
   } else if (st.kind == ALL) {
-    const Poly<11> poly = pinned(POW2_POLY);
     double sum = 0.0;
+    if (fabsf(top) < INF) {
+      const Poly<11> poly = pinned(POW2_POLY);
 #pragma unroll
-    for (int j = 0; j < N; ++j)
+      for (int j = 0; j < N; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const double y = l[j][e] == top ? 0.0 : ((double)l[j][e] - (double)top) * scale;  // 2^0 is 1, NaN weighs nothing
-        sum += power_of_two(y, poly);
-      }
+        for (int e = 0; e < 4; ++e) sum += power_of_two(((double)l[j][e] - (double)top) * scale, poly);  // NaN weighs nothing
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += l[j][e] == top ? 1.0 : 0.0;
+    }
     out.z = block_reduce<256>(sum, redd, [](double p, double q) { return p + q; });
   } else {
     const double g = grid_of(st);
@@ -557,31 +563,36 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
     out.off = !(fabsf(top * gf) < GRID_END);
     if (!out.off) {
       out.bucket = bucket_of(top, gf);
+      if (tid == 0) n_list = 0;
       for (int b = lane; b < BINS; b += 64) hist[wave][b] = 0;  // a wave's own: no barrier
       const bool mass = st.kind == NUCLEUS;
       const float first = (float)out.bucket;
       int limit = BINS;  // bins from there on have not counted all
       if (mass) {
-        // exp(f / 8), f in [-1, 0] (the float product's roundings beside), as a polynomial of degree six in f + 1/2 through its
-        // values at the Chebyshev points: to 2^-45, the bin takes 2^-37
-        const Poly<7> poly = pinned(Poly<7>{{4.97784668590196699e-09, 2.38947156470155655e-07, 9.55620375649920453e-06,
-                                             3.05798517364579050e-04, 7.33916455323328255e-03, 1.17426632851876683e-01,
-                                             9.39413062813475808e-01}});
+        // 2^36 exp(f / 8) + 2^52, f in [-1, 0] (the float product's roundings beside): the lower 52 bits are the bin's part.  A
+        // polynomial of degree six in f + 1/2 through the values at the Chebyshev points: to 2^-45, the bin takes 2^-37.
+        const Poly<7> poly = pinned(Poly<7>{{4.97784668590196699e-09 * 0x1p36, 2.38947156470155655e-07 * 0x1p36,
+                                             9.55620375649920453e-06 * 0x1p36, 3.05798517364579050e-04 * 0x1p36,
+                                             7.33916455323328255e-03 * 0x1p36, 1.17426632851876683e-01 * 0x1p36,
+                                             9.39413062813475808e-01 * 0x1p36 + 0x1p52}});
         const float from = bucket_start(out.bucket - (BINS - 2), g, top);  // below it the last bin
         float low = top;
-        auto add = [&](int rel, double w) __attribute__((always_inline)) {
-          const uint64_t v = (1ull << BIN_COUNT) + (__builtin_bit_cast(uint64_t, fma(w, 0x1p36, 0x1p52)) & ((1ull << 52) - 1));
-          atomicAdd((unsigned long long *)&hist[wave][rel], (unsigned long long)v);
+        char *const mine = reinterpret_cast<char *>(&hist[wave][0]);
+        auto add = [&](uint32_t place, double fixed) __attribute__((always_inline)) {
+          uint64_t v = __builtin_bit_cast(uint64_t, fixed);  // off with the exponent of 2^52, on with a count of one
+          v += (uint64_t)((1u << (BIN_COUNT - 32)) - 0x43300000u) << 32;
+          atomicAdd(reinterpret_cast<unsigned long long *>(mine + place), (unsigned long long)v);
         };
+        const float first8 = first * 8.f;
 #pragma unroll
         for (int j = 0; j < N; ++j)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const float v = l[j][e], fl = grid_place(v, gf);
+            const float v = l[j][e], fl = floorf(v * gf);
             low = fminf(low, v);
             if (!(v >= from)) continue;
-            const double f = fma((double)v, g, -0.5 - (double)fl);
-            add((int)(first - fl), poly(f));
+            const double f = fma((double)v, g, -(double)(fl + 0.5f));
+            add((uint32_t)(int)fmaf(fl, -8.f, first8), poly(f));
           }
         if (__any(low < from)) {
           const double last_edge = (double)(out.bucket - BINS + 2);
@@ -590,7 +601,7 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const float v = l[j][e];
-              if (v > -INF && v < from) add(BINS - 1, power_of_two_apart(((double)v * g - last_edge) * (LOG2E / 8.0)));
+              if (v > -INF && v < from) add((BINS - 1) * 8, fma(power_of_two_apart(((double)v * g - last_edge) * (LOG2E / 8.0)), 0x1p36, 0x1p52));
             }
         }
       } else {
@@ -632,41 +643,31 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
       out.cut = deep == 0 ? INT_MAX : deep >= BINS ? INT_MIN : out.bucket - deep + 1;
       if (deep > 0) {
         const float from = deep >= BINS ? -FLT_MAX : bucket_start(out.cut, g, top);
-        uint32_t flags = 0;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
+          uint64_t m[4];
           int c = 0;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const bool w = l[j][e] >= from;
-            flags |= (uint32_t)w << (j * 4 + e);
-            c += __popcll(__ballot(w));
+            m[e] = __ballot(l[j][e] >= from);
+            c += __popcll(m[e]);
           }
-          if (lane == 0) counts[j][wave] = c;
+          if (c == 0) continue;
+          int at = 0;
+          if (lane == 0) at = atomicAdd(&n_list, c);
+          at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (m[e] >> lane & 1) {
+              const int p = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m[e], 0));
+              list_l(a)[cell * ROOM + p] = l[j][e];
+              list_i(a)[cell * ROOM + p] = seg * SEG + (j * 256 + tid) * 4 + e;
+            }
+            at += __popcll(m[e]);
+          }
         }
         __syncthreads();
-        int base = 0;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-          int at = base;
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            if (w < wave) at += counts[j][w];
-            base += counts[j][w];
-          }
-          const uint32_t mine = flags >> (j * 4) & 15;
-          if (!__any(mine != 0)) continue;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) at += __popcll(__ballot(mine >> e & 1) & ((1ull << lane) - 1));
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (mine >> e & 1) {
-              list_l(a)[cell * ROOM + at] = l[j][e];
-              list_i(a)[cell * ROOM + at] = seg * SEG + (j * 256 + tid) * 4 + e;
-              ++at;
-            }
-        }
-        out.n = base;
+        out.n = n_list;
       }
     }
   }
@@ -693,8 +694,9 @@ template <class T> __device__ __forceinline__ T wave_before(T v) {  // sum over 
 
 // One workgroup per row.
 template <int BS>
-__global__ __launch_bounds__(BS, BS == 256 ? 3 : BS == 512 ? 2 : 4) void row_kernel(const SampleArgs a) {
-  __shared__ Shared sh;
+__global__ __launch_bounds__(BS, BS / 256) void row_kernel(const SampleArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char smem[];
+  Shared &sh = *reinterpret_cast<Shared *>(smem);
   const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, segs = a.segs;
   const float *x = a.logits + (size_t)row * a.V;
   const SegStat *stat = stats(a) + (size_t)row * segs;
@@ -717,15 +719,12 @@ __global__ __launch_bounds__(BS, BS == 256 ? 3 : BS == 512 ? 2 : 4) void row_ker
     const float u = a.u ? a.u[row] : 0.f;
     float thr = -INF;
     int last = INT_MAX;
-    const Source all{x, nullptr, a.V};
+    const Row all{x, a.V};
     const float hint = top - fminf(40.f * st.t, FLT_MAX);
     const float least = st.m > 0.f ? least_of(st.m, st.t, top, scale) : -INF;
     const double g = grid_of(st);
     const float gf = (float)g;
     const size_t cell0 = (size_t)row * segs * ROOM;
-    float *ml = mem_l(a) + cell0;
-    int32_t *mi = mem_i(a) + cell0;
-    const int room = segs * ROOM;
     int whole = INT_MIN, off = 0;  // the deepest bucket from which on every segment's list is whole; off the grid
     float lowest = -INF;           // the largest of the segments that are left out
 #pragma unroll
@@ -784,10 +783,10 @@ __global__ __launch_bounds__(BS, BS == 256 ? 3 : BS == 512 ? 2 : 4) void row_ker
         bool want[AHEAD];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) want[j] = l[j] >= from && l[j] < to;
-        collect(sh, want, l, i, ml, mi, room);
+        collect(sh, want, l, i);
       }
       __syncthreads();
-      return min(sh.n_mem, room);
+      return sh.n_mem;
     };
     // kept weight of the segments from the selection, exact whatever the order
     auto add_one = [&](float l, int idx) {
@@ -795,16 +794,15 @@ __global__ __launch_bounds__(BS, BS == 256 ? 3 : BS == 512 ? 2 : 4) void row_ker
       atomicAdd((unsigned long long *)&sh.seg_lo[idx / SEG], (unsigned long long)(fx & 0xffffffffu));
       atomicAdd((unsigned long long *)&sh.seg_hi[idx / SEG], (unsigned long long)(fx >> 32));
     };
-    auto add_kept = [&](const Source &s) {
+    auto add_kept = [&](const List &s) {
       for_each<BS>(s, [&](float l, int i) {
-        const int idx = s.idx[i];
-        if (l > thr || (l == thr && idx <= last)) add_one(l, idx);
+        if (l > thr || (l == thr && i <= last)) add_one(l, i);
       });
     };
-    // a selection of up to LIST elements lies in sh.list: cut there (see ranked), its kept ones added
-    auto cut_list = [&](int n, int k, double mass0, double rest) {
+    // of a list of up to LIST elements: see ranked; its kept ones added
+    auto cut_list = [&](const uint64_t *list, int n, int k, double mass0, double rest) {
       double kept;
-      const int n_kept = ranked<BS>(sh, n, k, (double)st.p, -1.0, mass0, rest, top, scale, kept);
+      const int n_kept = ranked<BS>(sh, list, n, k, (double)st.p, -1.0, mass0, rest, top, scale, kept);
       if (n_kept > 0) {
         thr = key_logit(sh.sorted[n_kept - 1]);
         last = key_index(sh.sorted[n_kept - 1]);
@@ -877,47 +875,62 @@ __global__ __launch_bounds__(BS, BS == 256 ? 3 : BS == 512 ? 2 : 4) void row_ker
       const int at = block_reduce<BS>(cnt > 0 && (before < target || tid == 0) ? tid : -1, sh.redi, [](int p, int q) { return max(p, q); });
       if (at == tid) { sh.before = before; sh.count = cnt; sh.sum = z - here; }
       __syncthreads();
-      const int b = first - at, n_b = sh.count;
+      int b = first - at, n_b = sh.count;
+      // the least weight may cut higher: then its bucket alone is looked at, from there on all stay
+      const bool by_least = st.m > 0.f && bucket_of(least, gf) > b;
+      if (by_least) {
+        b = bucket_of(least, gf);
+        n_b = (int)sh.h.cnt[first - b];
+      }
       const double mass0 = sh.before, rest = sh.sum + deep;
       // Where the target lies in what is deeper, the histogram does not tell; a bucket of too many is left to the row.
-      if (z >= target && at >= 0 && (b >= whole || n_b <= room)) {
-        const float lo_b = bucket_start(b, g, top), hi_b = b == first ? INF : bucket_start(b + 1, g, top);
-        Source mem{ml, mi, 0};
+      if (z >= target && at >= 0 && n_b <= MEM) {
+        const float lo_b = by_least ? least : bucket_start(b, g, top), hi_b = b == first ? INF : bucket_start(b + 1, g, top);
         if (b >= whole) {
-          mem.n = join(lo_b, hi_b);
+          (void)join(lo_b, hi_b);
         } else {
           // not in the lists: from the logits
-          constexpr int N = 4;
+          constexpr int N = 8;  // 64 KiB of a workgroup on their way: a row of 600 KB takes 2 us a request
+          f32x4u v[N], ahead[N];
+          auto request = [&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) ahead[j] = four(x, i0 + (j * BS + tid) * 4, a.V);
+          };
+          request(0);
           for (int i0 = 0; i0 < a.V; i0 += BS * 4 * N) {
-            float l[4 * N];
-            int idx[4 * N];
-            bool want[4 * N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = ahead[j];
+            if (i0 + BS * 4 * N < a.V) request(i0 + BS * 4 * N);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-              const int i = i0 + (j * BS + tid) * 4;
-              const f32x4u v = four(x, i, a.V);
+              float l[4];
+              int idx[4];
+              bool want[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                l[j * 4 + e] = v[e];
-                idx[j * 4 + e] = i + e;
-                want[j * 4 + e] = v[e] >= lo_b && v[e] < hi_b;
+                l[e] = v[j][e];
+                idx[e] = i0 + (j * BS + tid) * 4 + e;
+                want[e] = v[j][e] >= lo_b && v[j][e] < hi_b;
               }
+              collect(sh, want, l, idx);
             }
-            collect(sh, want, l, idx, ml, mi, room);
           }
           __syncthreads();
-          mem.n = min(sh.n_mem, room);
         }
-        // The bucket's weight anew from its elements: histogram and weights differ in the last bits, and among equal
-        // logits the border may fall on an element exactly.
-        if (mem.n <= LIST) {
-          cut_list(mem.n, INT_MAX, mass0, rest);
+        const List mem{sh.mem, sh.n_mem};
+        if (by_least) {
+          thr = least;
+          add_kept(mem);
+        } else if (mem.n <= LIST) {
+          // The bucket's weight anew from its elements: histogram and weights differ in the last bits, and among equal
+          // logits the border may fall on an element exactly.
+          cut_list(sh.mem, mem.n, INT_MAX, mass0, rest);
         } else {
           (void)cut<BS>(sh, mem, all, true, 0, (double)st.p, 0.0, mass0, rest, top, scale, lo_b, fminf(top, hi_b), thr, last);
           if (least > thr) { thr = least; last = INT_MAX; }
-          if (thr < hi_b) add_kept(mem);
+          add_kept(mem);
         }
-        if (thr < hi_b) {
+        {
           // of every segment: the buckets above, and what is kept of this one
           for (int c0 = wave * 64; c0 < segs * BINS; c0 += BS * AHEAD) {
             uint64_t v[AHEAD];
@@ -939,24 +952,54 @@ __global__ __launch_bounds__(BS, BS == 256 ? 3 : BS == 512 ? 2 : 4) void row_ker
               }
             }
           }
-        } else {
-          add_row();  // the least weight cuts higher
         }
         done = true;
       }
     } else if (st.kind == FEW && !off && whole != INT_MAX) {
-      const int n = join(whole == INT_MIN ? -INF : bucket_start(whole, g, top), INF);
-      const Source mem{ml, mi, n};
-      const bool in_list = n <= LIST && n >= st.k;
+      const float from = whole == INT_MIN ? -FLT_MAX : bucket_start(whole, g, top);
+      const int n = join(from, INF);
+      const List mem{sh.mem, min(n, MEM)};
+      const bool enough = n <= MEM && n >= st.k;
+      const uint64_t *list = sh.mem;
+      int few = n;  // elements of it
+      if (enough && n > LIST && st.k <= LIST) {
+        // too many to rank: those in front of and in the bucket, of a linear map, that the k-th lies in
+        const double places = top > from ? (BUCKETS - 1) / ((double)top - (double)from) : 0.0;
+        auto bucket = [&](float l) { return min(BUCKETS - 1, (int)(((double)top - (double)l) * places)); };
+        for (int b = tid; b < BUCKETS; b += BS) sh.h.cnt[b] = 0;
+        __syncthreads();
+        for_each<BS>(mem, [&](float l, int) { atomicAdd(&sh.h.cnt[bucket(l)], 1u); });
+        __syncthreads();
+        constexpr int PER = BUCKETS / BS;
+        int c[PER], own_c = 0, ctot, at = INT_MAX, upto = 0;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) own_c += c[e] = (int)sh.h.cnt[tid * PER + e];
+        int run = block_before<BS>(own_c, sh.redi, ctot);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+          if (run < st.k && run + c[e] >= st.k) { at = tid * PER + e; upto = run + c[e]; }
+          run += c[e];
+        }
+        if (at != INT_MAX) { sh.at = at; sh.count = upto; sh.n_list = 0; }  // one thread
+        __syncthreads();
+        few = sh.count;
+        list = sh.list;
+        if (few <= LIST)
+          for_each<BS>(mem, [&](float l, int i) {
+            if (bucket(l) <= sh.at) sh.list[atomicAdd(&sh.n_list, 1)] = rank_key(l, i);
+          });
+        __syncthreads();
+      }
+      const bool in_list = enough && few <= LIST;
       if (in_list) {
-        cut_list(n, st.k, 0.0, 0.0);
+        cut_list(list, few, st.k, 0.0, 0.0);
         done = thr > lowest;  // else a segment without a list may have one of them
-      } else if (n >= st.k) {
+      } else if (enough) {
         const double w = cut<BS>(sh, mem, all, false, st.k, -1.0, 0.0, 0.0, 0.0, top, scale, hint, top, thr, last);
         if (st.p < 1.f) (void)cut<BS>(sh, mem, all, true, 0, -1.0, (double)st.p * w, 0.0, 0.0, top, scale, hint, top, thr, last);
         done = thr > lowest;
         if (least > thr) { thr = least; last = INT_MAX; }
-      } else if ((st.k == INT_MAX || st.p >= 1.f) && st.m > 0.f && (whole == INT_MIN || bucket_of(least, gf) >= whole)) {
+      } else if (n <= MEM && n < st.k && (st.k == INT_MAX || st.p >= 1.f) && st.m > 0.f && (whole == INT_MIN || bucket_of(least, gf) >= whole)) {
         thr = least;
         done = true;
       }
@@ -1225,6 +1268,18 @@ __global__ __launch_bounds__(1024) void rest_draw_kernel(const SampleAcceptArgs 
   }
 }
 
+// the row kernel's LDS is more than a launch may ask for by default
+hipError_t ensure_row_lds() {
+  static bool raised[64] = {};
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+  if (raised[dev]) return hipSuccess;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&row_kernel<512>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Shared));
+  if (e == hipSuccess) raised[dev] = true;
+  return e;
+}
+
 }  // namespace
 
 hipError_t launch_sample_accept(const SampleAcceptArgs &a, hipStream_t s) {
@@ -1238,12 +1293,11 @@ hipError_t launch_sample_accept(const SampleAcceptArgs &a, hipStream_t s) {
 
 hipError_t launch_sample(const SampleArgs &a, hipStream_t s) {
   segment_kernel<<<a.M * a.segs, 256, 0, s>>>(a);
-  const hipError_t e = hipGetLastError();
+  hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  static const int BSX = getenv("SBS") ? atoi(getenv("SBS")) : 0;
-  if (BSX == 1024) row_kernel<1024><<<a.M, 1024, 0, s>>>(a);
-  else if (BSX == 512) row_kernel<512><<<a.M, 512, 0, s>>>(a);
-  else row_kernel<256><<<a.M, 256, 0, s>>>(a);
+  e = ensure_row_lds();
+  if (e != hipSuccess) return e;
+  row_kernel<512><<<a.M, 512, sizeof(Shared), s>>>(a);
   return hipGetLastError();
 }
 

@@ -142,6 +142,24 @@ size_t sf_kv_cache_bytes(const sf_ctx *ctx, int32_t which, int32_t B, int32_t ca
  * sf_verify_step / sf_accept_commit are used (plain autoregressive decoding, k = 0). */
 sf_status sf_bind(sf_ctx *ctx, const sf_target_weights *target, const sf_draft_weights *draft);
 
+/* A prefix that all sequences of a context's later steps continue (several continuations of one prompt): its keys and values,
+ * computed once, stand in front of every sequence and are read once per layer for all of them.  Positions count from its start:
+ * kv_len[b] (and host_len_upper, cap) are a sequence's own keys, its row i sits at position len + kv_len[b] + i.
+ *   tk, tv  caches of ONE sequence of capacity cap (multiple of 32), as a state of B = 1 has them after a prefill of the prefix
+ *   dk, dv  its draft caches; NULL when sf_draft_step is not called (SF_ESTATE there)
+ * all dev, 16-byte aligned, read only, borrowed until the next sf_set_prefix.  workspace: dev, 256-byte aligned,
+ * sf_prefix_workspace_bytes of the largest batch, block and capacity (0 in SF_F32 mode: NULL); the steps' order on one stream
+ * covers it as it does the state's.  A sequence that starts at kv_len 0 takes n_new = 1 and as hooks row the prefix's newest.
+ * SF_DRAFT_TWO_STAGE with a prefix is SF_EUNSUPPORTED.  prefix NULL: none any more. */
+typedef struct {
+  int32_t len, cap;
+  const void *tk, *tv, *dk, *dv;
+  void *workspace;
+  size_t workspace_bytes;
+} sf_prefix;
+size_t sf_prefix_workspace_bytes(const sf_ctx *ctx, int32_t B, int32_t k, int32_t cap);
+sf_status sf_set_prefix(sf_ctx *ctx, const sf_prefix *prefix);
+
 /* Multi-token generation (SpecFormer, Eq. dec1 / dec2 / enc).  Reads hooks rows [0,n_new[b]) --
  * the rows at positions [kv_len[b]-n_new[b], kv_len[b]) -- and:
  *   Grouped RMSNorm -> W_D -> K,V of the draft attention layer appended to the draft cache at

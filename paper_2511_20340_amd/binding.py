@@ -24,6 +24,7 @@ EXPORTS = [
     "sf_op_silu_mul", "sf_argmax_workspace_bytes", "sf_op_argmax", "sf_op_argmax_noalloc", "sf_op_accept", "sf_strerror",
     "sf_sample_workspace_bytes", "sf_sample_dist_bytes", "sf_op_sample", "sf_accept_sampled_workspace_bytes",
     "sf_op_accept_sampled", "sf_accept_commit_sampled", "sf_prefix_attention_workspace_bytes", "sf_op_prefix_attention",
+    "sf_prefix_workspace_bytes", "sf_set_prefix",
     "sf_last_hip_error", "sf_version",
     # include/specformer_aux.h
     "sf_tune_linear", "sf_linear_num_tiles", "sf_linear_config", "sf_linear_choice", "sf_tune_attention", "sf_calib_copy",
@@ -51,6 +52,11 @@ class DraftWeights(C.Structure):
 class State(C.Structure):
     _fields_ = [("B", i32), ("cap", i32), ("tk", vp), ("tv", vp), ("dk", vp), ("dv", vp), ("kv_len", vp),
                 ("pending", vp), ("hooks", vp), ("n_new", vp), ("cu_new", vp), ("workspace", vp),
+                ("workspace_bytes", sz)]
+
+
+class Prefix(C.Structure):
+    _fields_ = [("len", i32), ("cap", i32), ("tk", vp), ("tv", vp), ("dk", vp), ("dv", vp), ("workspace", vp),
                 ("workspace_bytes", sz)]
 
 
@@ -130,6 +136,9 @@ def lib():
     L.sf_prefix_attention_workspace_bytes.argtypes = [vp, i32, i32, i32, i32]
     L.sf_prefix_attention_workspace_bytes.restype = sz
     L.sf_op_prefix_attention.argtypes = [vp, vp, vp, vp, i32, i32, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp, sz, vp]
+    L.sf_prefix_workspace_bytes.argtypes = [vp, i32, i32, i32]
+    L.sf_prefix_workspace_bytes.restype = sz
+    L.sf_set_prefix.argtypes = [vp, P(Prefix)]
     L.sf_sample_workspace_bytes.argtypes = [i32, i32]
     L.sf_sample_workspace_bytes.restype = sz
     L.sf_sample_dist_bytes.argtypes = [i32]

@@ -37,6 +37,7 @@ struct sf_ctx {
   int verified_k = -1;
   // tuning overrides of this context (0 = automatic)
   int tune_tile = 0, tune_split = 0, tune_chunk = 0;
+  sf_prefix prefix{};  // len 0: none
 };
 
 namespace {
@@ -312,6 +313,27 @@ size_t kv_layer_bytes(const sf_model_cfg &m, int B, int cap) {
   return (size_t)B * m.n_kv_heads * cap * m.head_dim * esize(m.dtype);
 }
 
+// a layer's attention of a pass: over the context's shared prefix, if there is one.  which: 0 target layer `layer`, 1 draft
+sf_status check_prefix(const sf_ctx *c, int which, int B, int n_q, int len_upper) {
+  const sf_prefix &p = c->prefix;
+  if (p.len == 0) return SF_OK;
+  if (which == 1 && (!p.dk || !p.dv)) return SF_ESTATE;
+  return p.workspace_bytes < prefix_ws_bytes(c->tc, B, n_q, p.len, len_upper) ? SF_ECAPACITY : SF_OK;
+}
+void pass_attention(Run &r, const sf_model_cfg &m, int which, int layer, const void *q, const void *kc, const void *vc,
+                    const int32_t *kv_len, void *out, float *part_o, float *part_ml, int B, int n_q, int cap, int mode,
+                    int len_upper, const void *qkv, const float2 *table, const int32_t *order, const int32_t *slots, int plan_B) {
+  const sf_prefix &p = r.c->prefix;
+  if (p.len == 0) {
+    attention(r, m, q, kc, vc, kv_len, out, part_o, part_ml, B, n_q, cap, mode, len_upper, qkv, table, order, slots, plan_B);
+    return;
+  }
+  const size_t at = (size_t)layer * m.n_kv_heads * p.cap * m.head_dim * esize(m.dtype);
+  const char *pk = (const char *)(which == 0 ? p.tk : p.dk) + at, *pv = (const char *)(which == 0 ? p.tv : p.dv) + at;
+  prefix_attention(r, m, {pk, pv, p.len, p.cap, p.workspace}, q, kc, vc, kv_len, out, B, n_q, cap, mode, len_upper, qkv, table,
+                   order, slots);
+}
+
 // The sequences a pass runs over: rows and state arrays 0..n-1, whose caches are those of sequence slots[j] (null: j).
 // whole = false: of a verify pass the layers and their hooked states (no choices), of a draft step the context rows' K, V.
 struct Subset {
@@ -342,7 +364,7 @@ sf_status verify_pass(sf_ctx *c, const sf_state *st, int32_t k, const int32_t *d
   const sf_model_cfg &m = c->tc;
   const int B = sub.n, q = k + 1, M = B * q, cap = st->cap, qm = c->max_k + 1;
   if ((long)len_upper + q > cap) return SF_ECAPACITY;
-  if ((v = check_attn_shape(m, q)) != SF_OK) return v;
+  if ((v = check_attn_shape(m, q)) != SF_OK || (v = check_prefix(c, 0, B, q, len_upper)) != SF_OK) return v;
   const Arena A = plan(c, st->B, k, cap);
   char *ws = (char *)st->workspace;
   float *h = (float *)(ws + A.h);                                    // the residual stream
@@ -368,7 +390,7 @@ sf_status verify_pass(sf_ctx *c, const sf_state *st, int32_t k, const int32_t *d
   RopeArgs ra{};
   ra.qkv = qkv; ra.q_out = qr; ra.kv_len = st->kv_len; ra.n_new = nullptr; ra.table = (float2 *)(ws + A.table);
   ra.B = B; ra.n_q = q; ra.Hq = m.n_q_heads; ra.Hkv = m.n_kv_heads; ra.hd = m.head_dim; ra.cap = cap;
-  ra.kv_only = 0; ra.pos_mode = 0; ra.theta = m.rope_theta; ra.slots = sub.slots;
+  ra.kv_only = 0; ra.pos_mode = 0; ra.theta = m.rope_theta; ra.slots = sub.slots; ra.pos_base = c->prefix.len;
   // bf16, more attention workgroups than compute units: the table kernel also ranks the sequences by length, and the
   // attention launches of this call go by that order.  More than 512: the longest start first.  257 to 512 (what the chip
   // holds at once with a head dim of 128, two to a compute unit): the longest 256 workgroups' sequences come first, then the
@@ -386,8 +408,8 @@ sf_status verify_pass(sf_ctx *c, const sf_state *st, int32_t k, const int32_t *d
     ra.kc = kc; ra.vc = vc;
     // bf16: the attention kernel rotates Q and K and appends the block's K, V rows itself
     if (!bf) LAUNCH(K_ROPE, launch_rope_kv(ra, m.dtype, r.s));
-    attention(r, m, qr, kc, vc, st->kv_len, ao, (float *)(ws + A.part_o), (float *)(ws + A.part_ml), B, q, cap,
-              SF_MASK_CAUSAL, len_upper, bf ? qkv : nullptr, ra.table, ra.order, sub.slots, st->B);
+    pass_attention(r, m, 0, l, qr, kc, vc, st->kv_len, ao, (float *)(ws + A.part_o), (float *)(ws + A.part_ml), B, q, cap,
+                   SF_MASK_CAUSAL, len_upper, bf ? qkv : nullptr, ra.table, ra.order, sub.slots, st->B);
     // h += attention . W_O, and h += W_down . act: float sums; bf16 mode also refreshes the bf16 copy
     GemmExtra ex;
     ex.res_f32 = 1; ex.y2 = hb;
@@ -416,7 +438,9 @@ sf_status draft_pass(sf_ctx *c, const sf_state *st, int32_t k, int32_t mask, int
   const sf_model_cfg &m = c->dc;
   const int B = sub.n, cap = st->cap, qm = c->max_k + 1, Mh = B * qm, Ms = B * k;
   if ((long)len_upper + k > cap) return SF_ECAPACITY;
-  if ((v = check_attn_shape(m, k)) != SF_OK) return v;
+  if ((v = check_attn_shape(m, k)) != SF_OK || (v = check_prefix(c, 1, B, k, len_upper)) != SF_OK) return v;
+  // a sequence without a key of its own has its newest row in the prefix, which the two-stage context attention does not look for
+  if (two_stage && c->prefix.len > 0) return SF_EUNSUPPORTED;
   const sf_draft_weights &w = c->dw;
   if (two_stage && (!w.sa_norm || !w.sa_wqkv || !w.sa_wo)) return SF_ESTATE;
   if (two_stage && k > TK) return SF_EUNSUPPORTED;
@@ -444,7 +468,7 @@ sf_status draft_pass(sf_ctx *c, const sf_state *st, int32_t k, int32_t mask, int
   ra.qkv = kvc; ra.q_out = nullptr; ra.kc = st->dk; ra.vc = st->dv; ra.kv_len = st->kv_len; ra.n_new = st->n_new;
   ra.table = (float2 *)(ws + A.table);
   ra.B = B; ra.n_q = qm; ra.Hq = m.n_q_heads; ra.Hkv = m.n_kv_heads; ra.hd = m.head_dim; ra.cap = cap;
-  ra.kv_only = 1; ra.pos_mode = 1; ra.theta = m.rope_theta; ra.slots = sub.slots;
+  ra.kv_only = 1; ra.pos_mode = 1; ra.theta = m.rope_theta; ra.slots = sub.slots; ra.pos_base = c->prefix.len;
   // the same launch fills the slots' table (positions kv_len[b] + s) when they sit behind the cached context
   float2 *slot_table = ra.table + (size_t)Mh * (m.head_dim / 2);
   if (!two_stage && sub.whole) {
@@ -495,8 +519,8 @@ sf_status draft_pass(sf_ctx *c, const sf_state *st, int32_t k, int32_t mask, int
   if (two_stage) LAUNCH(K_ROPE, launch_rope_table(ra, r.s));  // slots at positions 0..k-1 of their own tile
   // bf16: the attention kernel rotates the slots' Q and K and appends their K, V rows itself
   if (!bf) LAUNCH(K_ROPE, launch_rope_kv(ra, m.dtype, r.s));
-  attention(r, m, qr, kc_s, vc_s, len_s, ao, part_o, part_ml, B, k, cap_s, mask, len_upper_s, bf ? qkv : nullptr,
-            ra.table, nullptr, two_stage ? nullptr : sub.slots, st->B);
+  pass_attention(r, m, 1, 0, qr, kc_s, vc_s, len_s, ao, part_o, part_ml, B, k, cap_s, mask, len_upper_s, bf ? qkv : nullptr,
+                 ra.table, nullptr, two_stage ? nullptr : sub.slots, st->B);
   ex.res_f32 = 1;
   gemm(r, m.dtype, ao, wo_s, nullptr, s0, s0, Ms, d, nq, 1, 0, 0, 0.f, &ex);
   norm_swiglu_in(r, m, s0, s0b, w.ffn_norm, w.w_gate_up, act, Ms, F, d);
@@ -580,7 +604,29 @@ sf_status sf_bind(sf_ctx *c, const sf_target_weights *t, const sf_draft_weights 
   // function attributes of the linear tiles that need more LDS than the default, set here so that the first launch
   // (possibly under stream capture) has nothing left to set; best effort -- a launch repeats the call and reports its error
   if (c->tc.dtype == SF_BF16) (void)gemm_prepare_device();
+  (void)sample_prepare_device();
   c->bound = true;
+  return SF_OK;
+}
+
+size_t sf_prefix_workspace_bytes(const sf_ctx *c, int32_t B, int32_t k, int32_t cap) {
+  if (!c || B < 1 || B > c->max_B || k < 0 || k > c->max_k || cap < TK || cap % TK) return 0;
+  const sf_model_cfg &m = c->tc;
+  if (m.dtype != SF_BF16) return 0;
+  const size_t n_rt = (m.n_q_heads / m.n_kv_heads * (k + 1) + 31) / 32, chunks = ((size_t)cap / TK + 15) / 16;
+  const size_t rows = prefix_rows_bound(B, k + 1, m.n_q_heads, m.n_kv_heads) + (size_t)B * m.n_kv_heads * chunks * n_rt * 32;
+  return up(rows * (m.head_dim + 2) * sizeof(float));
+}
+
+sf_status sf_set_prefix(sf_ctx *c, const sf_prefix *p) {
+  if (!c) return SF_EINVAL;
+  if (!p) { c->prefix = sf_prefix{}; return SF_OK; }
+  if (p->len < 1 || p->cap < TK || p->cap % TK || !p->tk || !p->tv || !p->dk != !p->dv) return SF_EINVAL;
+  if (((uintptr_t)p->tk | (uintptr_t)p->tv | (uintptr_t)p->dk | (uintptr_t)p->dv) % 16) return SF_EINVAL;
+  if (p->workspace ? ((uintptr_t)p->workspace) % ALIGN != 0 : c->tc.dtype == SF_BF16) return SF_EINVAL;
+  if (p->len > p->cap) return SF_ECAPACITY;
+  if ((size_t)p->cap * c->tc.head_dim * esize(c->tc.dtype) >= (1ull << 32)) return SF_EUNSUPPORTED;
+  c->prefix = *p;
   return SF_OK;
 }
 
@@ -605,6 +651,7 @@ sf_status sf_prefill_step(sf_ctx *c, const sf_state *st, int32_t k, const int32_
   if (n_seq < 1 || n_seq > st->B || !slots || !block_len || !target_ids || !accept_len || !out_tokens) return SF_EINVAL;
   if (k_draft < 0 || k_draft > c->max_k || (k_draft > 0 && !draft_tokens) || len_after < 0) return SF_EINVAL;
   if (k_draft > k && (v = check_state(c, st, k_draft, true)) != SF_OK) return v;  // room for the draft too, before the commit
+  if (last && k_draft > 0 && (v = check_prefix(c, 1, n_seq, k_draft, len_after)) != SF_OK) return v;
   if (last && (long)len_after + k_draft > st->cap) return SF_ECAPACITY;
   const Subset sub{n_seq, slots, last != 0};
   if ((v = verify_pass(c, st, k, tokens, len_upper, nullptr, target_ids, stream, sub)) != SF_OK) return v;

@@ -313,6 +313,12 @@ PrefixPlan prefix_plan(int B, int n_q, int Hq, int Hkv, int len) {
   return p;
 }
 
+size_t prefix_rows_bound(int B, int n_q, int Hq, int Hkv) {
+  const size_t R = (size_t)B * n_q * (Hq / Hkv);
+  // rows x chunks, with at most 512 / (Hkv x row tiles) chunks rounded up: one more of all rows, or 512 row tiles in all
+  return (size_t)Hkv * ((R + 127) / 128 * 128 + 128 * (512 / Hkv + 1));
+}
+
 hipError_t launch_prefix_bf16(const PrefixArgs &a, hipStream_t s) {
   return a.own.hd == 128 ? pick_prefix<128>(a, s) : pick_prefix<64>(a, s);
 }

@@ -118,7 +118,7 @@ __global__ __launch_bounds__(256) void rmsnorm_kernel(const TI *__restrict__ X, 
 __global__ void rope_table_kernel(float2 *__restrict__ table, const int32_t *__restrict__ kv_len,
                                   const int32_t *__restrict__ n_new, int B, int n_q, int half, int pos_mode,
                                   double log2_theta, int32_t *__restrict__ order, int pair_from, int32_t *__restrict__ dev_err,
-                                  int len_upper, int cap, float2 *__restrict__ table2, int n_q2) {
+                                  int len_upper, int cap, float2 *__restrict__ table2, int n_q2, int pos_base) {
   if (dev_err && blockIdx.x == 0) {
     // the launch grids of this step were sized from the host's bound: say so if a length breaks it
     const bool fwd = pos_mode == 0 || table2;        // rows that extend the sequences are part of this launch
@@ -152,7 +152,7 @@ __global__ void rope_table_kernel(float2 *__restrict__ table, const int32_t *__r
     table = table2; n_q = n_q2; pos_mode = 0;
   }
   const int i = idx % half, row = idx / half, b = row / n_q, r = row % n_q;
-  const int pos = pos_mode == 0 ? kv_len[b] + r : kv_len[b] - n_new[b] + r;
+  const int pos = pos_base + (pos_mode == 0 ? kv_len[b] + r : kv_len[b] - n_new[b] + r);
   const double inv_freq = exp2(-(double)(2 * i) / (double)(2 * half) * log2_theta);
   double s, c;
   sincos((double)pos * inv_freq, &s, &c);
@@ -318,7 +318,7 @@ hipError_t launch_rope_table(const RopeArgs &a, hipStream_t s) {
   const int n = a.B * (a.n_q + (a.table2 ? a.n_q2 : 0)) * half;
   rope_table_kernel<<<(n + 255) / 256 + (a.order ? 1 : 0), 256, 0, s>>>(a.table, a.kv_len, a.n_new, a.B, a.n_q, half,
                                                                         a.pos_mode, log2((double)a.theta), a.order, a.pair_from,
-                                                                        a.dev_err, a.len_upper, a.cap, a.table2, a.n_q2);
+                                                                        a.dev_err, a.len_upper, a.cap, a.table2, a.n_q2, a.pos_base);
   return hipGetLastError();
 }
 

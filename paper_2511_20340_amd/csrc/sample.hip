@@ -1291,6 +1291,8 @@ hipError_t launch_sample_accept(const SampleAcceptArgs &a, hipStream_t s) {
   return hipGetLastError();
 }
 
+hipError_t sample_prepare_device() { return ensure_row_lds(); }
+
 hipError_t launch_sample(const SampleArgs &a, hipStream_t s) {
   segment_kernel<<<a.M * a.segs, 256, 0, s>>>(a);
   hipError_t e = hipGetLastError();

@@ -112,6 +112,8 @@ struct PrefixPlan {
   int chunk_tiles, n_chunks;
 };
 PrefixPlan prefix_plan(int B, int n_q, int Hq, int Hkv, int len);
+// rows x chunks of the plan of any batch up to B and block up to n_q
+size_t prefix_rows_bound(int B, int n_q, int Hq, int Hkv);
 hipError_t launch_prefix_bf16(const PrefixArgs &a, hipStream_t s);          // partials of the prefix
 hipError_t launch_prefix_combine(const PrefixArgs &a, hipStream_t s);       // joins them with the own ones
 hipError_t launch_prefix_f32(const PrefixArgs &a, hipStream_t s);
@@ -210,6 +212,7 @@ struct RopeArgs {
   int len_upper = 0;
   int B, n_q, Hq, Hkv, hd, cap;
   int kv_only;   // rows carry only K,V
+  int pos_base = 0;  // keys in front of every sequence (a shared prefix): of the angles, not of the cache slots
   int pos_mode;  // 0: pos = kv_len[b]+i, all rows valid; 1: pos = kv_len[b]-n_new[b]+i, valid iff i<n_new[b]
   float theta;
 };
@@ -275,6 +278,7 @@ struct SampleArgs {
   char *ws;  // M * segs * SAMPLE_CELL_BYTES, 8-byte aligned
   int segs;  // (V + SAMPLE_SEG - 1) / SAMPLE_SEG
 };
+hipError_t sample_prepare_device();
 hipError_t launch_sample(const SampleArgs &a, hipStream_t s);
 struct SampleAcceptArgs {
   const int32_t *draft;       // [B][k]

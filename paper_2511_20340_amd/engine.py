@@ -67,6 +67,7 @@ class Engine:
                             _ptr(self.kv_len), _ptr(self.pending), _ptr(self.hooks), _ptr(self.n_new),
                             _ptr(self.cu_new), C.c_void_p(self._ws_ptr), wb)
         self.len_upper = 0          # host-side upper bound of max_b kv_len[b]
+        self._prefix = None
         self._pinned = False
         self._keep = []
 
@@ -231,6 +232,37 @@ class Engine:
         self._pinned = pinned
         if pinned:
             self.len_upper = self.cap - (self.max_k + 1)
+
+    def sf_set_prefix(self, one, length=None, start=True):
+        """From now on every sequence of the steps continues the first `length` (default: all) positions that `one`, an engine
+        of the same shapes with B = 1, has in its caches.  start: begin behind them, no keys of their own yet, with one's pending
+        token and newest hooked row.  one=None: no prefix any more."""
+        self._prefix = None
+        if one is None:
+            sfb.check(self.lib.sf_set_prefix(self.ctx, None), "sf_set_prefix", self.ctx)
+            return
+        shape = lambda e: {n: v for n, v in e.cfg.items() if n != "vocab"}  # noqa: E731
+        if one.B != 1 or shape(one) != shape(self) or one.dev != self.dev:
+            raise ValueError("sf_set_prefix: the prefix comes from an engine of the same shapes and device with B = 1")
+        held = int(one.kv_len[0].item())
+        length = held if length is None else int(length)
+        if not 1 <= length <= held:
+            raise ValueError(f"sf_set_prefix: {length} positions of a prefix that has {held}")
+        if start and length != held:
+            raise ValueError("sf_set_prefix: the newest hooked row is that of the prefix's end; start=False with a part of it")
+        with torch.cuda.device(self.dev):
+            nb = self.lib.sf_prefix_workspace_bytes(self.ctx, self.B, self.max_k, self.cap)
+            ws, p = self._workspace(nb)
+            pre = sfb.Prefix(length, one.cap, _ptr(one.tk), _ptr(one.tv), _ptr(one.dk), _ptr(one.dv), p if nb else None, nb)
+            sfb.check(self.lib.sf_set_prefix(self.ctx, C.byref(pre)), "sf_set_prefix", self.ctx)
+            self._prefix = (one, length, ws)
+            if start:
+                newest = max(int(one.n_new[0].item()) - 1, 0)
+                self.kv_len.zero_()
+                self.n_new.fill_(1)
+                self.pending.copy_(one.pending.expand(self.B))
+                self.hooks[:, 0] = one.hooks[0, newest]
+                self.len_upper = 0
 
     # ---- state helpers (plumbing) ------------------------------------------------------------
     def set_state(self, kv_len=None, pending=None, n_new=None):
@@ -569,6 +601,8 @@ class Engine:
             return _prefill_blocks(self, prompts, q, self.max_k)
         helper = Engine(self.cfg, self.B, self.cap, q - 1, device=self.dev, share_caches=self)
         helper.bind_shared(self, with_draft=self._D is not None)
+        if self._prefix is not None:
+            helper.sf_set_prefix(self._prefix[0], self._prefix[1], start=False)
         # row j of the helper is prompt order[j]; its K/V stay in the prompt's own cache slot
         lens = [len(p) for p in prompts]
         if len(lens) == self.B and min(lens) > 0:

@@ -1,4 +1,6 @@
 """Refusals of the shared-prefix attention, on the host: status codes before anything is launched."""
+import ctypes as C
+
 from paper_2511_20340_amd import binding as sfb
 from test_abi import cfg, create
 
@@ -34,5 +36,53 @@ def test_prefix_attention_validates_before_launching_anything():
     assert call(n_q=257, cap=512) == sfb.SF_EUNSUPPORTED   # 4 query heads per kv head x 257 rows > 1024
     assert call(B=1 << 16) == sfb.SF_EUNSUPPORTED
     assert call(pcap=1 << 25) == sfb.SF_EUNSUPPORTED       # a slab of 4 GiB
+    assert L.sf_last_hip_error(ctx) == 0
+    L.sf_destroy(ctx)
+
+
+def test_set_prefix_validates():
+    L = sfb.lib()
+    bf = dict(dtype=sfb.SF_BF16, n_q_heads=8, n_kv_heads=2, head_dim=64, d_model=512)
+    st, ctx = create(cfg(**bf), cfg(n_layers=1, **bf))
+    assert st == sfb.SF_OK
+    assert L.sf_prefix_workspace_bytes(ctx, 5, 4, 128) == 0 and L.sf_prefix_workspace_bytes(ctx, 4, 5, 128) == 0
+    assert L.sf_prefix_workspace_bytes(ctx, 4, 4, 100) == 0
+    need = L.sf_prefix_workspace_bytes(ctx, 4, 4, 128)
+    # room for any part of the batch, any block up to the largest, any prefix
+    for B in (1, 2, 3, 4):
+        for n_q in range(1, 6):
+            for P in (1, 33, 700, 5000, 100000):
+                assert L.sf_prefix_attention_workspace_bytes(ctx, B, n_q, P, 128 - n_q) <= need
+
+    def call(**kw):
+        a = dict(len=100, cap=128, tk=FAKE, tv=FAKE, dk=FAKE, dv=FAKE, workspace=FAKE, workspace_bytes=need)
+        a.update(kw)
+        return L.sf_set_prefix(ctx, C.byref(sfb.Prefix(**a)))
+    assert call() == sfb.SF_OK and call(dk=None, dv=None) == sfb.SF_OK
+    for bad in (dict(len=0), dict(len=-1), dict(cap=100), dict(cap=0), dict(tk=None), dict(tv=None), dict(dk=None), dict(dv=None),
+                dict(tk=FAKE + 8), dict(workspace=None), dict(workspace=FAKE + 16)):
+        assert call(**bad) == sfb.SF_EINVAL, bad
+    assert call(len=129) == sfb.SF_ECAPACITY
+    assert call(cap=1 << 25) == sfb.SF_EUNSUPPORTED
+    # steps look at the workspace and at the draft caches before anything is launched
+    tw, dw, s = sfb.TargetWeights(), sfb.DraftWeights(), sfb.State()
+    arr = (C.c_void_p * 2)(FAKE, FAKE)
+    for n, _ in sfb.TargetWeights._fields_:
+        setattr(tw, n, arr if n not in ("embed", "lm_head", "final_norm") else FAKE)
+    for n, _ in sfb.DraftWeights._fields_:
+        setattr(dw, n, FAKE)
+    assert L.sf_bind(ctx, C.byref(tw), C.byref(dw)) == sfb.SF_OK
+    for n in ("tk", "tv", "dk", "dv", "kv_len", "pending", "hooks", "n_new", "cu_new"):
+        setattr(s, n, FAKE)
+    s.B, s.cap, s.workspace, s.workspace_bytes = 4, 128, FAKE, L.sf_workspace_bytes(ctx, 4, 4, 128)
+    assert call(workspace_bytes=16) == sfb.SF_OK
+    assert L.sf_verify_step(ctx, C.byref(s), 4, FAKE, 0, None, FAKE, None) == sfb.SF_ECAPACITY
+    assert L.sf_draft_step(ctx, C.byref(s), 4, sfb.SF_MASK_BIDIR, 0, FAKE, None, None) == sfb.SF_ECAPACITY
+    assert call(dk=None, dv=None) == sfb.SF_OK
+    assert L.sf_draft_step(ctx, C.byref(s), 4, sfb.SF_MASK_BIDIR, 0, FAKE, None, None) == sfb.SF_ESTATE
+    assert call() == sfb.SF_OK
+    two_stage = sfb.SF_MASK_BIDIR | sfb.SF_DRAFT_TWO_STAGE
+    assert L.sf_draft_step(ctx, C.byref(s), 4, two_stage, 0, FAKE, None, None) == sfb.SF_EUNSUPPORTED
+    assert L.sf_set_prefix(None, None) == sfb.SF_EINVAL and L.sf_set_prefix(ctx, None) == sfb.SF_OK
     assert L.sf_last_hip_error(ctx) == 0
     L.sf_destroy(ctx)

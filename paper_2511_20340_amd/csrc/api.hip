@@ -293,11 +293,10 @@ void prefix_attention(Run &r, const sf_model_cfg &m, const Prefix &pre, const vo
   AttnArgs &a = p.own;
   a.q = q; a.qkv = qkv; a.table = table; a.order = order; a.slots = slots; a.kc = kc; a.vc = vc; a.kv_len = kv_len; a.out = out;
   a.B = B; a.n_q = n_q; a.Hq = m.n_q_heads; a.Hkv = m.n_kv_heads; a.hd = m.head_dim; a.cap = cap; a.mode = mode;
-  a.part_always = 1;
   p.pk = pre.k; p.pv = pre.v; p.len = pre.len; p.cap = pre.cap;
   if (m.dtype != SF_BF16) { LAUNCH(K_ATTN, launch_prefix_f32(p, r.s)); return; }
   const PrefixPlan pl = prefix_plan(B, n_q, a.Hq, a.Hkv, pre.len);
-  p.n_chunks = pl.n_chunks; p.chunk_tiles = pl.chunk_tiles; p.waves = pl.waves; p.rows = pl.rows;
+  p.n_chunks = pl.n_chunks; p.chunk_tiles = pl.chunk_tiles; p.rows = pl.rows;
   const int n_rt = (a.Hq / a.Hkv * n_q + 31) / 32;
   a.chunk_tiles = r.c->tune_chunk > 0 ? r.c->tune_chunk : attn_chunk_tiles(B * a.Hkv * n_rt, len_upper + n_q);
   a.n_chunks = ((len_upper + n_q + TK - 1) / TK + a.chunk_tiles - 1) / a.chunk_tiles;
@@ -305,7 +304,6 @@ void prefix_attention(Run &r, const sf_model_cfg &m, const Prefix &pre, const vo
   p.part_o = (float *)pre.ws; a.part_o = p.part_o + rows * a.hd;
   p.part_ml = a.part_o + own * a.hd; a.part_ml = p.part_ml + rows * 2;
   LAUNCH(K_ATTN, launch_prefix_bf16(p, r.s));
-  LAUNCH(K_ATTN, launch_attention_bf16(a, r.s));
   LAUNCH(K_ATTN_COMBINE, launch_prefix_combine(p, r.s));
 }
 

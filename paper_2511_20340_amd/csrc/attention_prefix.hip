@@ -7,34 +7,34 @@
 // the prefix the rows of ALL sequences that share a kv head are one matrix: its keys and values are read once per 32 * waves
 // rows instead of once per sequence, which makes that part a matrix product, bound by the matrix cores and the softmax between
 // the two products.
-#include "sf_internal.h"
+#include "attention_rows.h"
+#include <stdlib.h>
+#include <type_traits>
 
 namespace sf {
 namespace {
 
-constexpr float NEG_INF = -__builtin_huge_valf();
 constexpr int STEP_TILES = 2;  // 32-key tiles between two meetings of a workgroup's waves
 
 #ifdef __HIP_DEVICE_COMPILE__
 typedef __amdgpu_buffer_rsrc_t buffer_t;
 #endif
 
-// One workgroup: 32 * NW rows of one kv head, chunk_tiles tiles of the prefix.  The cache's tiles are MFMA operands as they
-// are: they go to LDS by direct loads, two stages of STEP_TILES tiles, and every wave reads the fragments it needs from there.
-template <int HD, int NW, int FUSE>
-__global__ __launch_bounds__(64 * NW, 2) void prefix_bf16_kernel(const bf16_t *__restrict__ Q, const void *Pk, const void *Pv,
-                                                                 float *__restrict__ part_o, float *__restrict__ part_ml, int R,
-                                                                 int rows, int n_q, int Hq, int Hkv, int len, int cap,
-                                                                 int chunk_tiles, int n_chunks, float scale_log2e,
-                                                                 const float2 *__restrict__ table) {
+// One workgroup: 128 rows of one kv head, chunk_tiles tiles of the prefix.  The cache's tiles are MFMA operands as they are: they
+// go to LDS by direct loads, two stages of STEP_TILES tiles, and every wave reads the fragments it needs from there.
+template <int HD> constexpr int PREFIX_LDS_BYTES = 2 * 2 * STEP_TILES * HD * 64;
+template <int HD, int FUSE>
+__device__ __forceinline__ void prefix_rows(const int id, char *smem, const bf16_t *__restrict__ Q, const void *Pk, const void *Pv,
+                                            float *__restrict__ part_o, float *__restrict__ part_ml, int R, int rows, int Hq,
+                                            int Hkv, int len, int cap, int chunk_tiles, int n_chunks, float scale_log2e,
+                                            const float2 *__restrict__ table) {
 #ifdef __HIP_DEVICE_COMPILE__
-  constexpr int KS = HD / 16, NT = HD / 32;
+  constexpr int KS = HD / 16, NT = HD / 32, NW = 4;
   constexpr int TILE = HD * 64;                    // bytes of a 32-key tile
   constexpr int STAGE = 2 * STEP_TILES * TILE;     // K tiles, then V tiles
   constexpr int LOADS = STAGE / 1024 / NW;         // of one wave for a stage
-  extern __shared__ __attribute__((aligned(1024))) char smem[];
   // kv heads fastest: eight of them are eight XCDs, each with its head's keys in an L2 of its own; then the rows of a chunk
-  const int g = blockIdx.x % Hkv, rt = blockIdx.x / Hkv % (rows / (32 * NW)), chunk = blockIdx.x / (Hkv * (rows / (32 * NW)));
+  const int tiles_r = rows / (32 * NW), g = id % Hkv, rt = id / Hkv % tiles_r, chunk = id / Hkv / tiles_r;
   const int G = Hq / Hkv;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
@@ -58,6 +58,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prefix_bf16_kernel(const bf16_t *_
   // Q^T operand: lane (n, h), k-step s holds features [(2s+h)*8, +8) of its row
   const int r = (rt * NW + wave) * 32 + n;
   const bool row_ok = r < R;
+  const bool idle = (rt * NW + wave) * 32 >= R;  // few rows: the other waves only load
   const int bi = row_ok ? r / G : 0, qh = g * G + (row_ok ? r % G : 0);  // bi = b * n_q + block row
   bf16x8 qf[KS];
   if (FUSE) {
@@ -83,38 +84,50 @@ __global__ __launch_bounds__(64 * NW, 2) void prefix_bf16_kernel(const bf16_t *_
   }
 
   f32x16 acc[NT];
+  float m_run = NEG_INF, l_run = 0.f;
 #pragma unroll
   for (int c = 0; c < NT; ++c)
 #pragma unroll
     for (int v = 0; v < 16; ++v) acc[c][v] = 0.f;
-  float m_run = NEG_INF, l_run = 0.f;
+  const int end = min(len, t1 * TK);  // keys of this chunk
 
-  for (int step = 0; step < steps; ++step) {
-    // this wave's loads of the stage have landed, everyone's have behind the barrier; the other stage has been read by all
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (step + 1 < steps) load(step + 1);
+  auto tiles = [&](int step, auto tail_c) __attribute__((always_inline)) {
+    constexpr bool TAIL = decltype(tail_c)::value;  // the stage holds keys behind the end: they may be anything (even NaN)
     const bf16x8 *kb = reinterpret_cast<const bf16x8 *>(smem + (step & 1) * STAGE) + lane;
     const bf16x8 *vb = kb + STEP_TILES * TILE / 16;
+    const int p0 = (t0 + step * STEP_TILES) * TK;
+    // All of the keys' fragments on their way, then products that do not wait for one another next to each other (fragment by
+    // fragment, as the compiler orders them by itself: 163 us where this takes 134).
+    bf16x8 kf[STEP_TILES][KS], vf[STEP_TILES][KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int t = 0; t < STEP_TILES; ++t) kf[t][s] = kb[(t * KS + s) * 64];
+    __builtin_amdgcn_sched_barrier(0);
     f32x16 sc[STEP_TILES];
 #pragma unroll
-    for (int t = 0; t < STEP_TILES; ++t) {
+    for (int t = 0; t < STEP_TILES; ++t)
 #pragma unroll
       for (int v = 0; v < 16; ++v) sc[t][v] = 0.f;
 #pragma unroll
-      for (int s = 0; s < KS; ++s)
-        sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kb[(t * KS + s) * 64], qf[s], sc[t], 0, 0, 0);
-    }
-    const int p0 = (t0 + step * STEP_TILES) * TK;
-    const int end = min(len, t1 * TK);       // keys of this chunk
-    const bool tail = p0 + STEP_TILES * TK > end;
-    float mx = NEG_INF;
-    if (tail) {
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int t = 0; t < STEP_TILES; ++t)
+        sc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[t][s], qf[s], sc[t], 0, 0, 0);
+    // the values' fragments arrive while the softmax runs
+#pragma unroll
+    for (int t = 0; t < STEP_TILES; ++t)
+#pragma unroll
+      for (int s = 0; s < KS; ++s) vf[t][s] = vb[(t * KS + s) * 64];
+    __builtin_amdgcn_sched_barrier(0);
+    if (TAIL) {
 #pragma unroll
       for (int t = 0; t < STEP_TILES; ++t)
 #pragma unroll
         for (int v = 0; v < 16; ++v)
           if (p0 + t * TK + c_row(v, h) >= end) sc[t][v] = NEG_INF;
     }
+    float mx = NEG_INF;
 #pragma unroll
     for (int t = 0; t < STEP_TILES; ++t)
 #pragma unroll
@@ -134,33 +147,48 @@ __global__ __launch_bounds__(64 * NW, 2) void prefix_bf16_kernel(const bf16_t *_
     }
     const float m_use = m_run == NEG_INF ? 0.f : m_run;
     bf16x8 pf[STEP_TILES][2];
-    float psum = 0.f;
+    float psum[2] = {0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < STEP_TILES; ++t)
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][v], scale_log2e, -m_use));
-        psum += p;
+        psum[v & 1] += p;
         pf[t][v >> 3][v & 7] = (__bf16)p;
       }
-    l_run += psum;
+    l_run += psum[0] + psum[1];
+    if (TAIL) {
+#pragma unroll
+      for (int t = 0; t < STEP_TILES; ++t)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          const uint4 w4 = __builtin_bit_cast(uint4, vf[t][s]);
+          uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (p0 + t * TK + 16 * (s / NT) + 8 * (e >> 2) + 4 * h + (e & 3) >= end) w[e >> 1] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
+          vf[t][s] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+        }
+    }
 #pragma unroll
     for (int t = 0; t < STEP_TILES; ++t)
 #pragma unroll
       for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int c = 0; c < NT; ++c) {
-          bf16x8 vf = vb[(t * KS + u * NT + c) * 64];
-          if (tail) {  // dead slots may hold anything (even NaN)
-            uint4 w4 = __builtin_bit_cast(uint4, vf);
-            uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (p0 + t * TK + 16 * u + 8 * (e >> 2) + 4 * h + (e & 3) >= end) w[e >> 1] &= (e & 1) ? 0x0000ffffu : 0xffff0000u;
-            vf = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
-          }
-          acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[t][u], acc[c], 0, 0, 0);
-        }
+        for (int c = 0; c < NT; ++c)
+          acc[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][u * NT + c], pf[t][u], acc[c], 0, 0, 0);
+  };
+  // this wave's loads of the stage have landed, everyone's have behind the barrier; the other stage has been read by all
+  auto meet = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+  const int whole = (end - t0 * TK) / (STEP_TILES * TK) == steps ? steps : steps - 1;  // steps without such keys
+  for (int step = 0; step < whole; ++step) {
+    meet();
+    if (step + 1 < steps) load(step + 1);
+    if (!idle) tiles(step, std::integral_constant<bool, false>{});
+  }
+  if (whole < steps) {
+    meet();
+    if (!idle) tiles(whole, std::integral_constant<bool, true>{});
   }
   const float l = l_run + __shfl_xor(l_run, 32);
   if (!row_ok) return;
@@ -173,6 +201,41 @@ __global__ __launch_bounds__(64 * NW, 2) void prefix_bf16_kernel(const bf16_t *_
       *reinterpret_cast<float4 *>(part_o + at * HD + 32 * c + 8 * j + 4 * h) =
           make_float4(acc[c][4 * j], acc[c][4 * j + 1], acc[c][4 * j + 2], acc[c][4 * j + 3]);
 #endif
+}
+
+// Both parts in one launch: the prefix's workgroups are bound by the matrix cores, those of the own keys by memory, and a
+// compute unit holds two workgroups, so the kinds are dealt out in turn, eight by eight (one to an XCD).
+struct PrefixKernelArgs {
+  const bf16_t *q;
+  const void *pk, *pv;
+  const uint4 *kc, *vc;
+  const int32_t *kv_len, *order, *slots;
+  const float2 *table;
+  float *pre_o, *pre_ml, *own_o, *own_ml;
+  int B, n_q, Hq, Hkv, cap, mode, own_tiles, own_chunks, n_rt;  // own keys
+  int len, pcap, pre_tiles, pre_chunks, rows;                   // prefix
+  int pre_blocks, own_blocks;
+  float scale_log2e;
+};
+template <int HD> constexpr int BOTH_LDS_BYTES = ATTN_LDS_BYTES<HD> > PREFIX_LDS_BYTES<HD> ? ATTN_LDS_BYTES<HD> : PREFIX_LDS_BYTES<HD>;
+template <int HD, int FUSE, int ONCE>
+__global__ __launch_bounds__(256, 2) void prefix_attn_kernel(const PrefixKernelArgs a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];
+  const int eight = blockIdx.x / 8, pre8 = (a.pre_blocks + 7) / 8, all8 = pre8 + (a.own_blocks + 7) / 8;
+  const int before = (int)((int64_t)eight * pre8 / all8), upto = (int)((int64_t)(eight + 1) * pre8 / all8);
+  if (upto > before) {
+    const int id = before * 8 + blockIdx.x % 8;
+    if (id < a.pre_blocks)
+      prefix_rows<HD, FUSE>(id, smem, a.q, a.pk, a.pv, a.pre_o, a.pre_ml, a.B * a.n_q * (a.Hq / a.Hkv), a.rows, a.Hq, a.Hkv, a.len,
+                            a.pcap, a.pre_tiles, a.pre_chunks, a.scale_log2e, a.table);
+    return;
+  }
+  const int id = (eight - before) * 8 + blockIdx.x % 8;
+  if (id >= a.own_blocks) return;
+  const int y = a.Hkv * a.n_rt;
+  attn_rows<HD, FUSE, ONCE, 1>(make_uint3(id % a.own_chunks, id / a.own_chunks % y, id / a.own_chunks / y), reinterpret_cast<float *>(smem),
+                               a.q, a.kc, a.vc, a.kv_len, nullptr, a.own_o, a.own_ml, a.n_q, a.Hq, a.Hkv, a.cap, a.mode,
+                               a.own_tiles, a.own_chunks, a.n_rt, a.scale_log2e, a.table, a.order, a.slots);
 }
 
 // Joins the partials of the prefix and of the own keys: 32 lanes per query row, 8 rows per workgroup, every lane HD / 32
@@ -284,29 +347,35 @@ __global__ __launch_bounds__(256) void prefix_f32_kernel(const float *__restrict
   }
 }
 
-template <int HD, int NW, int FUSE> hipError_t run_prefix(const PrefixArgs &a, hipStream_t s) {
-  constexpr int LDS = 2 * 2 * STEP_TILES * HD * 64;
-  const AttnArgs &o = a.own;
-  prefix_bf16_kernel<HD, NW, FUSE><<<o.Hkv * (a.rows / (32 * NW)) * a.n_chunks, 64 * NW, LDS, s>>>(
-      (const bf16_t *)(FUSE ? o.qkv : o.q), a.pk, a.pv, a.part_o, a.part_ml, o.B * o.n_q * (o.Hq / o.Hkv), a.rows, o.n_q, o.Hq,
-      o.Hkv, a.len, a.cap, a.chunk_tiles, a.n_chunks, 1.4426950408889634f / sqrtf((float)HD), o.table);
+template <int HD, int FUSE, int ONCE> hipError_t run_prefix(const PrefixKernelArgs &a, hipStream_t s) {
+  static bool raised[64] = {};  // LDS beyond what a launch may ask for by default
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return hipErrorInvalidDevice;
+  if (!raised[dev]) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&prefix_attn_kernel<HD, FUSE, ONCE>),
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, BOTH_LDS_BYTES<HD>);
+    if (e != hipSuccess) return e;
+    raised[dev] = true;
+  }
+  const int blocks = ((a.pre_blocks + 7) / 8 + (a.own_blocks + 7) / 8) * 8;
+  prefix_attn_kernel<HD, FUSE, ONCE><<<blocks, 256, BOTH_LDS_BYTES<HD>, s>>>(a);
   return hipGetLastError();
 }
 
-template <int HD> hipError_t pick_prefix(const PrefixArgs &a, hipStream_t s) {
-  if (a.own.qkv) return a.waves == 4 ? run_prefix<HD, 4, 1>(a, s) : a.waves == 2 ? run_prefix<HD, 2, 1>(a, s) : run_prefix<HD, 1, 1>(a, s);
-  return a.waves == 4 ? run_prefix<HD, 4, 0>(a, s) : a.waves == 2 ? run_prefix<HD, 2, 0>(a, s) : run_prefix<HD, 1, 0>(a, s);
+template <int HD> hipError_t pick_prefix(const PrefixKernelArgs &a, bool fuse, hipStream_t s) {
+  if (fuse) return a.n_rt == 1 ? run_prefix<HD, 1, 1>(a, s) : run_prefix<HD, 1, 0>(a, s);
+  return a.n_rt == 1 ? run_prefix<HD, 0, 1>(a, s) : run_prefix<HD, 0, 0>(a, s);
 }
 
 }  // namespace
 
 PrefixPlan prefix_plan(int B, int n_q, int Hq, int Hkv, int len) {
   const int R = B * n_q * (Hq / Hkv), n_tiles = (len + TK - 1) / TK;
+  static const int SL = getenv("PS") ? atoi(getenv("PS")) : 512;
   PrefixPlan p;
-  p.waves = R <= 32 ? 1 : R <= 64 ? 2 : 4;
-  const int row_tiles = (R + 32 * p.waves - 1) / (32 * p.waves);
-  p.rows = row_tiles * 32 * p.waves;
-  const int want = (512 + Hkv * row_tiles - 1) / (Hkv * row_tiles);
+  const int row_tiles = (R + 127) / 128;
+  p.rows = row_tiles * 128;
+  const int want = (SL + Hkv * row_tiles - 1) / (Hkv * row_tiles);
   p.chunk_tiles = (n_tiles + want - 1) / want;
   if (p.chunk_tiles < 8) p.chunk_tiles = 8;
   p.n_chunks = (n_tiles + p.chunk_tiles - 1) / p.chunk_tiles;
@@ -320,7 +389,19 @@ size_t prefix_rows_bound(int B, int n_q, int Hq, int Hkv) {
 }
 
 hipError_t launch_prefix_bf16(const PrefixArgs &a, hipStream_t s) {
-  return a.own.hd == 128 ? pick_prefix<128>(a, s) : pick_prefix<64>(a, s);
+  const AttnArgs &o = a.own;
+  PrefixKernelArgs k{};
+  k.q = (const bf16_t *)(o.qkv ? o.qkv : o.q);
+  k.pk = a.pk; k.pv = a.pv; k.kc = (const uint4 *)o.kc; k.vc = (const uint4 *)o.vc;
+  k.kv_len = o.kv_len; k.order = o.order; k.slots = o.slots; k.table = o.table;
+  k.pre_o = a.part_o; k.pre_ml = a.part_ml; k.own_o = o.part_o; k.own_ml = o.part_ml;
+  k.B = o.B; k.n_q = o.n_q; k.Hq = o.Hq; k.Hkv = o.Hkv; k.cap = o.cap; k.mode = o.mode;
+  k.own_tiles = o.chunk_tiles; k.own_chunks = o.n_chunks; k.n_rt = (o.Hq / o.Hkv * o.n_q + 31) / 32;
+  k.len = a.len; k.pcap = a.cap; k.pre_tiles = a.chunk_tiles; k.pre_chunks = a.n_chunks; k.rows = a.rows;
+  k.pre_blocks = o.Hkv * (a.rows / 128) * a.n_chunks;
+  k.own_blocks = o.n_chunks * o.Hkv * k.n_rt * o.B;
+  k.scale_log2e = 1.4426950408889634f / sqrtf((float)o.hd);
+  return o.hd == 128 ? pick_prefix<128>(k, o.qkv != nullptr, s) : pick_prefix<64>(k, o.qkv != nullptr, s);
 }
 
 hipError_t launch_prefix_combine(const PrefixArgs &a, hipStream_t s) {

@@ -89,7 +89,6 @@ struct AttnArgs {
   int B, n_q, Hq, Hkv, hd, cap, mode;
   int chunk_tiles;  // tiles of 32 keys per workgroup chunk
   int n_chunks;     // grid.x
-  int part_always;  // bf16 only: no output, a partial of every chunk
 };
 int attn_chunk_tiles(int groups, int keys_upper);  // groups = B * Hkv * row tiles
 size_t attn_workspace_bytes(int B, int Hkv, int hd, int G, int n_q, int len_upper);
@@ -104,18 +103,17 @@ struct PrefixArgs {
   const void *pk, *pv;       // the prefix: one layer's cache of one sequence
   int len, cap;              // its keys, the cache's capacity
   float *part_o, *part_ml;   // bf16: [Hkv][chunks][rows][hd], [Hkv][chunks][rows][2]
-  int n_chunks, chunk_tiles, waves, rows;  // of the plan
+  int n_chunks, chunk_tiles, rows;  // of the plan
 };
 struct PrefixPlan {
-  int waves;        // of a workgroup, 32 rows each
-  int rows;         // (b, block row, query head of the kv head), padded to whole workgroups
+  int rows;  // (b, block row, query head of the kv head), padded to whole workgroups
   int chunk_tiles, n_chunks;
 };
 PrefixPlan prefix_plan(int B, int n_q, int Hq, int Hkv, int len);
 // rows x chunks of the plan of any batch up to B and block up to n_q
 size_t prefix_rows_bound(int B, int n_q, int Hq, int Hkv);
-hipError_t launch_prefix_bf16(const PrefixArgs &a, hipStream_t s);          // partials of the prefix
-hipError_t launch_prefix_combine(const PrefixArgs &a, hipStream_t s);       // joins them with the own ones
+hipError_t launch_prefix_bf16(const PrefixArgs &a, hipStream_t s);     // partials of the prefix and of the own keys
+hipError_t launch_prefix_combine(const PrefixArgs &a, hipStream_t s);  // joins them
 hipError_t launch_prefix_f32(const PrefixArgs &a, hipStream_t s);
 
 struct GemmArgs {

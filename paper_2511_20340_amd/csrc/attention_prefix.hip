@@ -8,7 +8,7 @@
 // rows instead of once per sequence, which makes that part a matrix product, bound by the matrix cores and the softmax between
 // the two products.
 #include "attention_rows.h"
-#include <stdlib.h>
+#include <algorithm>
 #include <type_traits>
 
 namespace sf {
@@ -203,8 +203,8 @@ __device__ __forceinline__ void prefix_rows(const int id, char *smem, const bf16
 #endif
 }
 
-// Both parts in one launch: the prefix's workgroups are bound by the matrix cores, those of the own keys by memory, and a
-// compute unit holds two workgroups, so the kinds are dealt out in turn, eight by eight (one to an XCD).
+// Both parts in one launch: the prefix's workgroups, bound by the matrix cores, first, those of the own keys, bound by memory and
+// short, where they leave room and at the end (dealt out in turn, or the own ones first: 171 and 157 us where this takes 147).
 struct PrefixKernelArgs {
   const bf16_t *q;
   const void *pk, *pv;
@@ -221,17 +221,12 @@ template <int HD> constexpr int BOTH_LDS_BYTES = ATTN_LDS_BYTES<HD> > PREFIX_LDS
 template <int HD, int FUSE, int ONCE>
 __global__ __launch_bounds__(256, 2) void prefix_attn_kernel(const PrefixKernelArgs a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];
-  const int eight = blockIdx.x / 8, pre8 = (a.pre_blocks + 7) / 8, all8 = pre8 + (a.own_blocks + 7) / 8;
-  const int before = (int)((int64_t)eight * pre8 / all8), upto = (int)((int64_t)(eight + 1) * pre8 / all8);
-  if (upto > before) {
-    const int id = before * 8 + blockIdx.x % 8;
-    if (id < a.pre_blocks)
-      prefix_rows<HD, FUSE>(id, smem, a.q, a.pk, a.pv, a.pre_o, a.pre_ml, a.B * a.n_q * (a.Hq / a.Hkv), a.rows, a.Hq, a.Hkv, a.len,
-                            a.pcap, a.pre_tiles, a.pre_chunks, a.scale_log2e, a.table);
+  if ((int)blockIdx.x < a.pre_blocks) {
+    prefix_rows<HD, FUSE>(blockIdx.x, smem, a.q, a.pk, a.pv, a.pre_o, a.pre_ml, a.B * a.n_q * (a.Hq / a.Hkv), a.rows, a.Hq, a.Hkv,
+                          a.len, a.pcap, a.pre_tiles, a.pre_chunks, a.scale_log2e, a.table);
     return;
   }
-  const int id = (eight - before) * 8 + blockIdx.x % 8;
-  if (id >= a.own_blocks) return;
+  const int id = blockIdx.x - a.pre_blocks;
   const int y = a.Hkv * a.n_rt;
   attn_rows<HD, FUSE, ONCE, 1>(make_uint3(id % a.own_chunks, id / a.own_chunks % y, id / a.own_chunks / y), reinterpret_cast<float *>(smem),
                                a.q, a.kc, a.vc, a.kv_len, nullptr, a.own_o, a.own_ml, a.n_q, a.Hq, a.Hkv, a.cap, a.mode,
@@ -357,8 +352,7 @@ template <int HD, int FUSE, int ONCE> hipError_t run_prefix(const PrefixKernelAr
     if (e != hipSuccess) return e;
     raised[dev] = true;
   }
-  const int blocks = ((a.pre_blocks + 7) / 8 + (a.own_blocks + 7) / 8) * 8;
-  prefix_attn_kernel<HD, FUSE, ONCE><<<blocks, 256, BOTH_LDS_BYTES<HD>, s>>>(a);
+  prefix_attn_kernel<HD, FUSE, ONCE><<<a.pre_blocks + a.own_blocks, 256, BOTH_LDS_BYTES<HD>, s>>>(a);
   return hipGetLastError();
 }
 
@@ -371,13 +365,15 @@ template <int HD> hipError_t pick_prefix(const PrefixKernelArgs &a, bool fuse, h
 
 PrefixPlan prefix_plan(int B, int n_q, int Hq, int Hkv, int len) {
   const int R = B * n_q * (Hq / Hkv), n_tiles = (len + TK - 1) / TK;
-  static const int SL = getenv("PS") ? atoi(getenv("PS")) : 512;
   PrefixPlan p;
   const int row_tiles = (R + 127) / 128;
   p.rows = row_tiles * 128;
-  const int want = (SL + Hkv * row_tiles - 1) / (Hkv * row_tiles);
-  p.chunk_tiles = (n_tiles + want - 1) / want;
-  if (p.chunk_tiles < 8) p.chunk_tiles = 8;
+  // As many workgroups as the chip holds at once (two to a compute unit), not more: a chunk more costs its partials.  128 x 5
+  // rows, 8192 keys, in 1, 2, 3, 4 chunks: 173, 157, 163, 161 us with the join; 37 x 4 rows, 1500 keys: 38, 27, 25, 25, in 5
+  // and 6 26 and 26.  Below 12 tiles to a chunk nothing is gained unless the rows are one tile and all is latency.
+  const int want = std::max(1, 512 / (Hkv * row_tiles));
+  p.chunk_tiles = std::max((n_tiles + want - 1) / want, row_tiles == 1 ? 8 : 12);
+  p.chunk_tiles = (p.chunk_tiles + STEP_TILES - 1) / STEP_TILES * STEP_TILES;
   p.n_chunks = (n_tiles + p.chunk_tiles - 1) / p.chunk_tiles;
   return p;
 }

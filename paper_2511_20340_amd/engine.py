@@ -2,6 +2,7 @@
 tensors and hands their pointers to the C ABI.  Method names mirror the C entry points; no step
 of the path is computed here (torch is used for memory, streams and host<->device copies only).
 """
+import contextlib
 import ctypes as C
 
 import numpy as np
@@ -12,6 +13,10 @@ from . import binding as sfb
 
 def _ptr(t):
     return C.c_void_p(t.data_ptr()) if t is not None else None
+
+
+def _addr(t):
+    return t.data_ptr() if t is not None else None
 
 
 def _stream():
@@ -252,8 +257,8 @@ class Engine:
             raise ValueError("sf_set_prefix: the newest hooked row is that of the prefix's end; start=False with a part of it")
         with torch.cuda.device(self.dev):
             nb = self.lib.sf_prefix_workspace_bytes(self.ctx, self.B, self.max_k, self.cap)
-            ws, p = self._workspace(nb)
-            pre = sfb.Prefix(length, one.cap, _ptr(one.tk), _ptr(one.tv), _ptr(one.dk), _ptr(one.dv), p if nb else None, nb)
+            ws, at = self._workspace(nb)
+            pre = sfb.Prefix(length, one.cap, _addr(one.tk), _addr(one.tv), _addr(one.dk), _addr(one.dv), at if nb else None, nb)
             sfb.check(self.lib.sf_set_prefix(self.ctx, C.byref(pre)), "sf_set_prefix", self.ctx)
             self._prefix = (one, length, ws)
             if start:
@@ -330,13 +335,14 @@ class Engine:
                 raise ValueError(f"{what}: pk, pv must be slabs of one sequence of a capacity of whole tiles, kc, vc at least B slabs")
         if len_upper is None:
             len_upper = int(kv_len.max().item())
-        with torch.cuda.device(self.dev):
+        with self._on_device():
             need = self.lib.sf_prefix_attention_workspace_bytes(self.ctx, B, n_q, prefix_len, len_upper)
-            ws, p = self._workspace(need)
+            ws, at = self._workspace(need)
             out = torch.empty_like(q)
-            sfb.check(self.lib.sf_op_prefix_attention(self.ctx, _ptr(q), _ptr(pk), _ptr(pv), prefix_len, pk.numel() // row,
-                                                      _ptr(kc), _ptr(vc), _ptr(kv_len), B, n_q, self.cap, mask, len_upper,
-                                                      _ptr(out), p, need, _stream()), what, self.ctx)
+            sfb.check(self.lib.sf_op_prefix_attention(self.ctx, q.data_ptr(), pk.data_ptr(), pv.data_ptr(), prefix_len,
+                                                      pk.numel() // row, kc.data_ptr(), vc.data_ptr(), kv_len.data_ptr(), B, n_q,
+                                                      self.cap, mask, len_upper, out.data_ptr(), at, need,
+                                                      torch.cuda.current_stream().cuda_stream), what, self.ctx)
         return out
 
     def linear_workspace(self, M):
@@ -481,29 +487,37 @@ class Engine:
         return ids
 
     # ---- sampled decoding --------------------------------------------------------------------
+    # Calls of a few microseconds: what they check and set up on the host is kept short.
     def _need(self, what, name, t, shape, dtype):
         """t is a dense tensor of that shape and type on the engine's device."""
-        if not isinstance(t, torch.Tensor) or tuple(t.shape) != tuple(shape) or t.dtype != dtype or not t.is_contiguous():
+        if not isinstance(t, torch.Tensor) or t.shape != shape or t.dtype != dtype or not t.is_contiguous():
             raise ValueError(f"{what}: {name} must be a dense {dtype} tensor of shape {tuple(shape)}")
-        if t.device != self._cuda_dev():
-            raise ValueError(f"{what}: {name} is on {t.device}, the engine on {self._cuda_dev()}")
+        if t.get_device() != self._index():
+            raise ValueError(f"{what}: {name} is on {t.device}, the engine on {self.dev}")
 
-    def _cuda_dev(self):
-        return self.dev if self.dev.index is not None else torch.device("cuda", torch.cuda.current_device())
+    def _index(self):
+        return self.dev.index if self.dev.index is not None else torch.cuda.current_device()
+
+    def _on_device(self):
+        """The engine's device as the current one for a call's launches and allocations; nothing to do where it is."""
+        if self.dev.index is None or torch.cuda.current_device() == self.dev.index:
+            return contextlib.nullcontext()
+        return torch.cuda.device(self.dev)
 
     def _sampling(self, what, n, temperature, top_k, top_p, min_p):
-        s = sfb.Sampling()
+        if temperature is None and top_k is None and top_p is None and min_p is None:
+            return None
         for name, t, dtype in (("temperature", temperature, torch.float32), ("top_k", top_k, torch.int32),
                                ("top_p", top_p, torch.float32), ("min_p", min_p, torch.float32)):
             if t is not None:
                 self._need(what, name, t, (n,), dtype)
-                setattr(s, name, t.data_ptr())
-        return s
+        return C.byref(sfb.Sampling(_addr(temperature), _addr(top_k), _addr(top_p), _addr(min_p)))
 
     def _workspace(self, nbytes):
-        """(tensor, aligned pointer) of a call's workspace, from the allocator of the current stream."""
+        """(tensor, aligned address) of a call's workspace, from the allocator of the current stream."""
         ws = torch.empty(nbytes + 256, dtype=torch.uint8, device=self.dev)
-        return ws, C.c_void_p(ws.data_ptr() + (-ws.data_ptr()) % 256)
+        at = ws.data_ptr()
+        return ws, at + (-at) % 256
 
     def sf_op_sample(self, logits, u, temperature=None, top_k=None, top_p=None, min_p=None, group=1, want_prob=False,
                      want_dist=False, ids=None):
@@ -519,17 +533,19 @@ class Engine:
         par = self._sampling(what, -(-M // group), temperature, top_k, top_p, min_p)
         if ids is not None:
             self._need(what, "ids", ids, (M,), torch.int32)
-        with torch.cuda.device(self.dev):
+        with self._on_device():
             if ids is None:
                 ids = torch.empty(M, dtype=torch.int32, device=self.dev)
             prob = torch.empty(M, dtype=torch.float32, device=self.dev) if want_prob else None
             dist = torch.empty(self.lib.sf_sample_dist_bytes(M), dtype=torch.uint8, device=self.dev) if want_dist else None
             nb = self.lib.sf_sample_workspace_bytes(M, V)
-            ws, p = self._workspace(nb)
-            sfb.check(self.lib.sf_op_sample(self.ctx, _ptr(logits), M, V, group, C.byref(par), _ptr(u), _ptr(ids), _ptr(prob),
-                                            _ptr(dist), p, nb, _stream()), what, self.ctx)
-        out = (ids,) + ((prob,) if want_prob else ()) + ((dist,) if want_dist else ())
-        return out if len(out) > 1 else ids
+            ws, at = self._workspace(nb)
+            sfb.check(self.lib.sf_op_sample(self.ctx, logits.data_ptr(), M, V, group, par, u.data_ptr(), ids.data_ptr(),
+                                            _addr(prob), _addr(dist), at, nb, torch.cuda.current_stream().cuda_stream),
+                      what, self.ctx)
+        if not (want_prob or want_dist):
+            return ids
+        return (ids,) + ((prob,) if want_prob else ()) + ((dist,) if want_dist else ())
 
     def _accept_sampled(self, what, call, k, V, draft, target_logits, u_accept, u_sample, settings, draft_logits, draft_dist,
                         accept_out, tokens_out):
@@ -551,13 +567,14 @@ class Engine:
             self._need(what, "accept_out", accept_out, (B,), i32)
         if tokens_out is not None:
             self._need(what, "tokens_out", tokens_out, (B, k + 1), i32)
-        with torch.cuda.device(self.dev):
+        with self._on_device():
             acc = accept_out if accept_out is not None else torch.empty(B, dtype=i32, device=self.dev)
             out = tokens_out if tokens_out is not None else torch.empty(B, k + 1, dtype=i32, device=self.dev)
             nb = self.lib.sf_accept_sampled_workspace_bytes(B, k, V)
-            ws, p = self._workspace(nb)
-            sfb.check(call(_ptr(draft), _ptr(target_logits), C.byref(par), _ptr(draft_logits), _ptr(draft_dist),
-                           _ptr(u_accept), _ptr(u_sample), acc, out, p, nb), what, self.ctx)
+            ws, at = self._workspace(nb)
+            sfb.check(call((_addr(draft), target_logits.data_ptr(), par, _addr(draft_logits), _addr(draft_dist),
+                            _addr(u_accept), u_sample.data_ptr(), acc.data_ptr(), out.data_ptr()),
+                           (at, nb, torch.cuda.current_stream().cuda_stream)), what, self.ctx)
         return acc, out
 
     def sf_op_accept_sampled(self, k, draft, target_logits, u_accept, u_sample, temperature=None, top_k=None, top_p=None,
@@ -567,10 +584,9 @@ class Engine:
         sf_op_sample left for them, or neither for greedy drafts.  -> (accept_len [B], out_tokens [B,k+1])"""
         V = target_logits.shape[-1]
 
-        def call(d, t, par, dl, dd, ua, us, acc, out, ws, nb):
-            return self.lib.sf_op_accept_sampled(self.ctx, self.B, k, V, d, t, par, dl, dd, ua, us, _ptr(acc), _ptr(out),
-                                                 _ptr(self.kv_len), _ptr(self.pending), _ptr(self.n_new), _ptr(self.cu_new),
-                                                 ws, nb, _stream())
+        def call(args, ws):
+            return self.lib.sf_op_accept_sampled(self.ctx, self.B, k, V, *args, self.st.kv_len, self.st.pending, self.st.n_new,
+                                                 self.st.cu_new, *ws)
         return self._accept_sampled("sf_op_accept_sampled", call, k, V, draft, target_logits, u_accept, u_sample,
                                     (temperature, top_k, top_p, min_p), draft_logits, draft_dist, None, None)
 
@@ -578,9 +594,8 @@ class Engine:
                                  min_p=None, draft_logits=None, draft_dist=None, accept_out=None, tokens_out=None):
         """sf_accept_commit at temperature > 0: arguments as sf_op_accept_sampled, target_logits as sf_verify_step returned
         them."""
-        def call(d, t, par, dl, dd, ua, us, acc, out, ws, nb):
-            return self.lib.sf_accept_commit_sampled(self.ctx, C.byref(self.st), k, d, t, par, dl, dd, ua, us, _ptr(acc),
-                                                     _ptr(out), ws, nb, _stream())
+        def call(args, ws):
+            return self.lib.sf_accept_commit_sampled(self.ctx, C.byref(self.st), k, *args, *ws)
         r = self._accept_sampled("sf_accept_commit_sampled", call, k, self.V, draft, target_logits, u_accept, u_sample,
                                  (temperature, top_k, top_p, min_p), draft_logits, draft_dist, accept_out, tokens_out)
         if not self._pinned:

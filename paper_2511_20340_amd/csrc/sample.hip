@@ -25,7 +25,7 @@ namespace sf {
 namespace {
 
 constexpr int BUCKETS = 1024;    // of one refinement of the ranking
-constexpr int LIST = 512;        // elements that are ranked one by one
+constexpr int LIST = 1536;       // elements that are ranked one by one: a count of a thousand, with what shares its last bucket
 constexpr int MEM = 8192;        // elements of a row that LDS has room for
 constexpr int STEP = 256;        // elements per partial sum of the draw: four to a lane of a wave
 constexpr int SEG = SAMPLE_SEG, MAX_SEGS = SAMPLE_MAX_VOCAB / SEG;
@@ -208,7 +208,7 @@ struct List {
 struct Shared {
   struct {
     uint32_t cnt[BUCKETS];
-    uint64_t lo[BUCKETS], hi[BUCKETS];  // weight * 2^62, its lower 32 bits and the rest
+    uint64_t lo[2 * BUCKETS];  // weight * 2^62: its lower 32 bits, and BUCKETS on the rest
   } h;
   uint64_t mem[MEM], list[LIST], sorted[LIST];
   double seg[MAX_SEGS], step[SEG / STEP];  // kept weight of the segments, of a segment's steps
@@ -253,18 +253,67 @@ template <int BS, class F> __device__ __forceinline__ void for_each(const List &
 
 __device__ __forceinline__ double from_fixed(uint64_t lo, uint64_t hi) { return (double)hi * 0x1p-30 + (double)lo * 0x1p-62; }
 
-// sh.sorted = list[0, n) by falling key.  An element's place is the number of larger ones: 512 elements take 1.5 us, a
-// network of exchanges with a barrier in each of its 45 steps takes ten.
+// sh.sorted = list[0, n) by falling key.  An element's place is the number of larger ones; a wave's comparison of 64 elements
+// with one is four cycles of LDS, so that few are compared with all, and of more (COUNT) each with those of its own bucket of
+// a linear map (of equal logits there is one).  A network of exchanges with a barrier in each of its steps is slower from 512 on.
 template <int BS> __device__ void sort_list(Shared &sh, const uint64_t *list, int n) {
-  constexpr int PARTS = BS > LIST ? BS / LIST : 1;  // lanes that share an element's comparisons
-  for (int e = threadIdx.x / PARTS; e < n; e += BS / PARTS) {
-    const uint64_t key = list[e];
-    int place = 0;
+  constexpr int COUNT = 320, EACH = (LIST + BS - 1) / BS, PER = BUCKETS / BS;
+  const int tid = threadIdx.x;
+  if (n <= COUNT) {
+    for (int e = tid; e < n; e += BS) {
+      const uint64_t key = list[e];
+      int place = 0;
 #pragma unroll 8
-    for (int j = threadIdx.x % PARTS; j < n; j += PARTS) place += list[j] > key;
+      for (int j = 0; j < n; ++j) place += list[j] > key;
+      sh.sorted[place] = key;
+    }
+    __syncthreads();
+    return;
+  }
+  uint64_t key[EACH];
+  float mn = INF, mx = -INF;
 #pragma unroll
-    for (int o = 1; o < PARTS; o <<= 1) place += __shfl_xor(place, o);
-    if (threadIdx.x % PARTS == 0) sh.sorted[place] = key;
+  for (int e = 0; e < EACH; ++e) {
+    const int i = e * BS + tid;
+    key[e] = i < n ? list[i] : 0;
+    if (i < n) { mn = fminf(mn, key_logit(key[e])); mx = fmaxf(mx, key_logit(key[e])); }
+  }
+  for (int b = tid; b < BUCKETS; b += BS) sh.h.cnt[b] = 0;
+  mn = block_reduce<BS>(mn, (float *)sh.redu, [](float p, float q) { return fminf(p, q); });
+  mx = block_reduce<BS>(mx, (float *)sh.redu, [](float p, float q) { return fmaxf(p, q); });
+  const bool map = mn > -INF && mx < INF && mn < mx;
+  const double places = map ? (BUCKETS - 1) / ((double)mx - (double)mn) : 0.0;
+  int bucket[EACH], at[EACH];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    bucket[e] = map ? min(BUCKETS - 1, (int)(((double)mx - (double)key_logit(key[e])) * places)) : 0;
+    if (e * BS + tid < n) at[e] = (int)atomicAdd(&sh.h.cnt[bucket[e]], 1u);
+  }
+  __syncthreads();
+  // counts to starts
+  int c[PER], own = 0, all;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) own += c[e] = (int)sh.h.cnt[tid * PER + e];
+  int run = block_before<BS>(own, sh.redi, all);
+#pragma unroll
+  for (int e = 0; e < PER; ++e) {
+    sh.h.cnt[tid * PER + e] = (uint32_t)run;
+    run += c[e];
+  }
+  __syncthreads();
+  uint64_t *const grouped = sh.h.lo;
+  static_assert(LIST <= 2 * BUCKETS, "the list by buckets");
+#pragma unroll
+  for (int e = 0; e < EACH; ++e)
+    if (e * BS + tid < n) grouped[(int)sh.h.cnt[bucket[e]] + at[e]] = key[e];
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    if (e * BS + tid >= n) continue;
+    const int lo = (int)sh.h.cnt[bucket[e]], hi = bucket[e] + 1 < BUCKETS ? (int)sh.h.cnt[bucket[e] + 1] : n;
+    int place = lo;
+    for (int j = lo; j < hi; ++j) place += grouped[j] > key[e];
+    sh.sorted[place] = key[e];
   }
   __syncthreads();
 }
@@ -357,22 +406,25 @@ __device__ double cut(Shared &sh, const Source &s, const Row &ties, bool by_mass
     const double places = hi > lo ? (BUCKETS - 2) / ((double)hi - (double)lo) : 0.0;
     auto bucket = [&](float l) {
       if (whole || l == hi) return 0;
-      if (l < lo || hi == INF) return BUCKETS - 1;
+      if (l < lo || l == -INF || hi == INF) return BUCKETS - 1;
       return min(BUCKETS - 2, (int)(((double)hi - (double)l) * places));
     };
     auto inside = [&](float l, int i) { return l <= hi && (below || l >= lo) && kept(l, i); };
     int at = 0, n_at = s.n;
     if (!whole) {
-      for (int x = tid; x < BUCKETS; x += BS) { sh.h.cnt[x] = 0; sh.h.lo[x] = 0; sh.h.hi[x] = 0; }
+      for (int x = tid; x < BUCKETS; x += BS) { sh.h.cnt[x] = 0; sh.h.lo[x] = 0; sh.h.lo[BUCKETS + x] = 0; }
       __syncthreads();
+      int minus = 0;  // -inf weighs nothing: counted apart, a mask's thousands would queue for one address
       for_each<BS>(s, [&](float l, int i) {
         if (!inside(l, i)) return;
+        if (l == -INF && l < hi) { ++minus; return; }
         const int b = bucket(l);
         atomicAdd(&sh.h.cnt[b], 1u);
         const uint64_t fx = (uint64_t)(weight(l, top, scale) * 0x1p62);
         atomicAdd((unsigned long long *)&sh.h.lo[b], (unsigned long long)(fx & 0xffffffffu));
-        atomicAdd((unsigned long long *)&sh.h.hi[b], (unsigned long long)(fx >> 32));
+        atomicAdd((unsigned long long *)&sh.h.lo[BUCKETS + b], (unsigned long long)(fx >> 32));
       });
+      if (minus) atomicAdd(&sh.h.cnt[BUCKETS - 1], (uint32_t)minus);
       __syncthreads();
       // running counts and weights; each thread has PER consecutive buckets
       int c[PER], cs = 0;
@@ -381,7 +433,7 @@ __device__ double cut(Shared &sh, const Source &s, const Row &ties, bool by_mass
       for (int e = 0; e < PER; ++e) {
         const int b = tid * PER + e;
         c[e] = b < BUCKETS ? (int)sh.h.cnt[b] : 0;
-        w[e] = b < BUCKETS ? from_fixed(sh.h.lo[b], sh.h.hi[b]) : 0.0;
+        w[e] = b < BUCKETS ? from_fixed(sh.h.lo[b], sh.h.lo[BUCKETS + b]) : 0.0;
         cs += c[e]; ws += w[e];
       }
       int ctot;
@@ -760,14 +812,14 @@ __global__ __launch_bounds__(BS, BS / 256) void row_kernel(const SampleArgs a) {
       if (lane == 0) sh.n_mem = 0;
     }
     __syncthreads();
-    // selects what lies in [from, to) of the segments' lists
-    auto join = [&](float from, float to) {
-      constexpr int AHEAD = 4;
-      for (int t0 = wave; t0 < pieces; t0 += BS / 64 * AHEAD) {
-        float l[AHEAD];
-        int i[AHEAD];
+    // f(l[], i[]) for the entries of the segments' lists, four pieces of a wave at a time; NaN: not there
+    constexpr int PIECES = 4;
+    auto visit = [&](auto f) {
+      for (int t0 = wave; t0 < pieces; t0 += BS / 64 * PIECES) {
+        float l[PIECES];
+        int i[PIECES];
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
+        for (int j = 0; j < PIECES; ++j) {
           const int t = t0 + j * (BS / 64);
           l[j] = __builtin_nanf(""); i[j] = 0;
           if (t < pieces) {
@@ -780,13 +832,35 @@ __global__ __launch_bounds__(BS, BS / 256) void row_kernel(const SampleArgs a) {
             }
           }
         }
-        bool want[AHEAD];
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j) want[j] = l[j] >= from && l[j] < to;
-        collect(sh, want, l, i);
+        f(l, i);
       }
       __syncthreads();
+    };
+    // selects what lies in [from, to) of the segments' lists
+    auto join = [&](float from, float to) {
+      visit([&](const float (&l)[PIECES], const int (&i)[PIECES]) {
+        bool want[PIECES];
+#pragma unroll
+        for (int j = 0; j < PIECES; ++j) want[j] = l[j] >= from && l[j] < to;
+        collect(sh, want, l, i);
+      });
       return sh.n_mem;
+    };
+    // The bucket of 1024, by rising number, that the k-th lies in: sh.at, and how many lie up to its end: sh.count (at: BUCKETS if
+    // there are fewer than k).
+    auto bucket_of_kth = [&]() {
+      constexpr int PER = BUCKETS / BS;
+      int c[PER], own_c = 0, ctot;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) own_c += c[e] = (int)sh.h.cnt[tid * PER + e];
+      int run = block_before<BS>(own_c, sh.redi, ctot);
+      if (tid == 0 && ctot < st.k) sh.at = BUCKETS;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) {
+        if (run < st.k && run + c[e] >= st.k) { sh.at = tid * PER + e; sh.count = run + c[e]; }
+        run += c[e];
+      }
+      __syncthreads();
     };
     // kept weight of the segments from the selection, exact whatever the order
     auto add_one = [&](float l, int idx) {
@@ -957,9 +1031,24 @@ __global__ __launch_bounds__(BS, BS / 256) void row_kernel(const SampleArgs a) {
       }
     } else if (st.kind == FEW && !off && whole != INT_MAX) {
       const float from = whole == INT_MIN ? -FLT_MAX : bucket_start(whole, g, top);
-      const int n = join(from, INF);
+      int n = join(from, INF);
+      if (n > MEM && st.k <= MEM / 2) {
+        // more than there is room for: the bucket of the grid that the k-th lies in, and what lies from there on
+        const int first = bucket_of(top, gf);
+        for (int b = tid; b < BUCKETS; b += BS) sh.h.cnt[b] = 0;
+        __syncthreads();
+        visit([&](const float (&l)[PIECES], const int (&)[PIECES]) {
+#pragma unroll
+          for (int j = 0; j < PIECES; ++j)
+            if (l[j] >= from) atomicAdd(&sh.h.cnt[min(BUCKETS - 1, first - bucket_of(l[j], gf))], 1u);
+        });
+        if (tid == 0) sh.n_mem = 0;
+        bucket_of_kth();
+        if (sh.at < BUCKETS - 1) n = join(fmaxf(from, bucket_start(first - sh.at, g, top)), INF);
+      }
       const List mem{sh.mem, min(n, MEM)};
-      const bool enough = n <= MEM && n >= st.k;
+      // lists of all there is and a share of its weight: the count drops none that weighs anything
+      const bool enough = n <= MEM && (n >= st.k || (whole == INT_MIN && st.p < 1.f));
       const uint64_t *list = sh.mem;
       int few = n;  // elements of it
       if (enough && n > LIST && st.k <= LIST) {
@@ -967,21 +1056,11 @@ __global__ __launch_bounds__(BS, BS / 256) void row_kernel(const SampleArgs a) {
         const double places = top > from ? (BUCKETS - 1) / ((double)top - (double)from) : 0.0;
         auto bucket = [&](float l) { return min(BUCKETS - 1, (int)(((double)top - (double)l) * places)); };
         for (int b = tid; b < BUCKETS; b += BS) sh.h.cnt[b] = 0;
+        if (tid == 0) sh.n_list = 0;
         __syncthreads();
         for_each<BS>(mem, [&](float l, int) { atomicAdd(&sh.h.cnt[bucket(l)], 1u); });
         __syncthreads();
-        constexpr int PER = BUCKETS / BS;
-        int c[PER], own_c = 0, ctot, at = INT_MAX, upto = 0;
-#pragma unroll
-        for (int e = 0; e < PER; ++e) own_c += c[e] = (int)sh.h.cnt[tid * PER + e];
-        int run = block_before<BS>(own_c, sh.redi, ctot);
-#pragma unroll
-        for (int e = 0; e < PER; ++e) {
-          if (run < st.k && run + c[e] >= st.k) { at = tid * PER + e; upto = run + c[e]; }
-          run += c[e];
-        }
-        if (at != INT_MAX) { sh.at = at; sh.count = upto; sh.n_list = 0; }  // one thread
-        __syncthreads();
+        bucket_of_kth();
         few = sh.count;
         list = sh.list;
         if (few <= LIST)

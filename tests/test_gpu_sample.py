@@ -109,6 +109,20 @@ def test_temperatures_at_the_limits(eng):
     check(eng, np.tile(x, (len(per), 1)), per, rng.random(len(per)).astype(np.float32))
 
 
+@pytest.mark.parametrize("V", [700, 12095, 33000, 131072])
+def test_large_counts(eng, V):
+    """Counts around what is ranked one by one, what LDS has room for and what a row has unmasked."""
+    rng = np.random.default_rng(V + 2)
+    x = (rng.normal(size=(4, V)) * 1.8).astype(np.float32)
+    x[1, rng.random(V) < 0.9] = -np.inf
+    x[2] = np.round(x[2] * 8) / 8
+    x[3, rng.random(V) < 0.995] = -np.inf
+    per = [(t, k, p, m) for k in (300, 512, 1000, 1535, 1537, 4096, 4097, 8200, 20000)
+           for t, p, m in ((1.0, 1.0, 0.0), (0.7, 0.9, 0.0), (3.0, 0.98, 0.0), (1.3, 0.95, 0.05))]
+    for row in x:
+        check(eng, np.tile(row, (len(per), 1)), per, rng.random(len(per)).astype(np.float32))
+
+
 def test_numbers_outside_the_unit_interval(eng):
     x = np.random.default_rng(4).normal(size=1000).astype(np.float32)
     x[990:] = -np.inf

@@ -312,6 +312,7 @@ template <int BS> __device__ void sort_list(Shared &sh, const uint64_t *list, in
     if (e * BS + tid >= n) continue;
     const int lo = (int)sh.h.cnt[bucket[e]], hi = bucket[e] + 1 < BUCKETS ? (int)sh.h.cnt[bucket[e] + 1] : n;
     int place = lo;
+#pragma unroll 8  // of equal logits the bucket is long
     for (int j = lo; j < hi; ++j) place += grouped[j] > key[e];
     sh.sorted[place] = key[e];
   }

@@ -13,6 +13,11 @@
 // into by the segments' kept weights, and reads that one again for the token.  What a segment had no room for (a flat row's
 // nucleus of tens of thousands) is read from the logits again, for that row alone.
 //
+// What bounds them: the first launch the vector instructions, at half the rate that the logits could be read with when all
+// rows ask for a nucleus (640 rows of 152064: 127 us, 3.1 TB/s) and 3.3 TB/s for settings of all kinds (256 of 128256: 40 us);
+// the second one the latency of a row's dozen dependent steps, 17 to 25 us, a compute unit to a row (640 rows 116 us, 256 rows
+// 49, one row 14).  A single workgroup per row, which reads the row in each of its steps, takes 691 us for the 640 rows.
+//
 // Weights are doubles: in a vocabulary of 150000 tokens a float sum is off by more than many tokens weigh, and the token
 // next to a border would hang on the order of the sum.  Where weights are summed by atomics they are integers (multiples of
 // 2^-62 in two halves, or of 2^-36 of a bucket's edge), so that the order does not matter there either: a row's result has the
@@ -353,8 +358,8 @@ template <int BS> __device__ int nth_equal(Shared &sh, const Row &s, float v, in
 // weight itself.  mass0: weight of elements that rank in front and are not among them.  Returns how many stay (sh.sorted) and
 // their weight, mass0 with it.
 template <int BS>
-__device__ int ranked(Shared &sh, const uint64_t *list, int n, int k, double share, double target, double mass0, double rest, float top, double scale,
-                      double &kept) {
+__device__ int ranked(Shared &sh, const uint64_t *list, int n, int k, double share, double target, double mass0, double rest,
+                      float top, double scale, double &kept) {
   constexpr int EACH = LIST / BS > 0 ? LIST / BS : 1;
   const int tid = threadIdx.x;
   sort_list<BS>(sh, list, n);
@@ -385,8 +390,9 @@ __device__ int ranked(Shared &sh, const uint64_t *list, int n, int k, double sha
 
 // Cuts the ranking of the elements that are kept so far (l > thr or l == thr and index <= last): by_mass, behind the last
 // element in front of which less than `target` of weight lies (share >= 0: that share of the weight of these and `rest`, what
-// else there is); else behind the k best.  mass0: weight of elements that rank in front of all of these and are not among them.  thr and last receive the last
-// kept element; returns the kept weight.  ties: where the j-th of equal elements is looked up (s may be in any order).  lo_hint: nothing of interest is expected below; hi: nothing lies above.
+// else there is); else behind the k best.  mass0: weight of elements that rank in front of all of these and are not among
+// them.  thr and last receive the last kept element; returns the kept weight.  ties: where the j-th of equal elements is looked up
+// (s may be in any order).  lo_hint: nothing of interest is expected below; hi: nothing lies above.
 //
 // A refinement sorts the elements of an interval of logits into buckets by a linear map (it never puts a smaller logit in
 // front of a larger one), finds the bucket of the cut from the running counts and weights, and goes on with that bucket's
@@ -1102,7 +1108,8 @@ __global__ __launch_bounds__(BS, BS / 256) void row_kernel(const SampleArgs a) {
       thr = -INF; last = INT_MAX;
       double w = -1.0;
       if (st.k != INT_MAX) w = cut<BS>(sh, all, all, false, st.k, -1.0, 0.0, 0.0, 0.0, top, scale, hint, top, thr, last);
-      if (st.p < 1.f) (void)cut<BS>(sh, all, all, true, 0, w < 0.0 ? (double)st.p : -1.0, (double)st.p * w, 0.0, 0.0, top, scale, hint, top, thr, last);
+      if (st.p < 1.f)
+        (void)cut<BS>(sh, all, all, true, 0, w < 0.0 ? (double)st.p : -1.0, (double)st.p * w, 0.0, 0.0, top, scale, hint, top, thr, last);
       if (least > thr) { thr = least; last = INT_MAX; }
       add_row();
     }

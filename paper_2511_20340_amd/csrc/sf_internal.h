@@ -248,11 +248,10 @@ hipError_t launch_accept(const AcceptArgs &a, hipStream_t s);
 
 // ---- sampling (sample.hip) --------------------------------------------------------------------
 constexpr int SAMPLE_MAX_VOCAB = 1 << 20, SAMPLE_MAX_ROWS = 1 << 20;
-constexpr int SAMPLE_SEG = 8192;  // tokens of a row that one workgroup sums; 256 threads hold a row's segments
+constexpr int SAMPLE_SEG = 8192;  // tokens of a row that one workgroup of the first launch holds in registers
 // of every (row, segment) in the workspace: its summary, a histogram of 64-bit bins, room for tokens (logit and index)
 constexpr int SAMPLE_BINS = 256, SAMPLE_ROOM = 512, SAMPLE_STAT_BYTES = 32;
 constexpr size_t SAMPLE_CELL_BYTES = SAMPLE_STAT_BYTES + SAMPLE_BINS * 8 + SAMPLE_ROOM * 8;
-static_assert(SAMPLE_MAX_VOCAB / SAMPLE_SEG <= 256 && SAMPLE_SEG / 64 <= 256, "one thread per segment, one per step of a segment");
 // What is kept of a row: the tokens with l > thr, or l == thr and an index <= last; their weights exp((l - top) / temp) sum
 // up to z.  id, prob: the token drawn.
 struct SampleDist {

@@ -1051,7 +1051,7 @@ void accept_sampled(Run &r, int B, int k, int V, const AcceptSampled &s, int32_t
   SampleArgs a{s.target_logits, B * (k + 1), V, k + 1, par.temperature, par.top_k, par.top_p, par.min_p,
                nullptr, nullptr, nullptr, dist, ws + p.sample, (V + SAMPLE_SEG - 1) / SAMPLE_SEG};
   LAUNCH(K_ARGMAX, launch_sample(a, r.s));
-  SampleAcceptArgs c{s.draft, s.target_logits, dist, k > 0 ? s.draft_logits : nullptr, (const SampleDist *)s.draft_dist,
+  SampleAcceptArgs c{s.draft, s.target_logits, dist, ws + p.sample, k > 0 ? s.draft_logits : nullptr, (const SampleDist *)s.draft_dist,
                      s.u_accept, s.u_sample, (double *)(ws + p.part), (int32_t *)(ws + p.tokens),
                      (int32_t *)(ws + p.accept), (int32_t *)(ws + p.accept) + B, B, k, V};
   LAUNCH(K_ACCEPT, launch_sample_accept(c, r.s));

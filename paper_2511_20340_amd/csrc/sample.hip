@@ -548,7 +548,7 @@ struct SegStat {
   int32_t cut;    // the list holds all of the segment's elements from this bucket on; INT_MAX: not even the first
   int32_t n;      // entries of the list, in any order
   int32_t off;    // the grid does not reach the values
-  double z;       // ALL: sum of weights against the segment's largest
+  double z;       // ALL: sum of weights against the segment's largest.  Behind a row kernel that draws no token: the kept weight
 };
 static_assert(sizeof(SegStat) == SAMPLE_STAT_BYTES, "workspace");
 
@@ -1121,6 +1121,11 @@ __global__ __launch_bounds__(BS, BS / 256) void row_kernel(const SampleArgs a) {
     const double z0 = wave_reduce(w0, [](double p, double q) { return p + q; });
     const double z = z0 + wave_reduce(w1, [](double p, double q) { return p + q; });
     d.thr = thr; d.last = last; d.z = z;
+    if (!a.u && wave == 0) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+        if (lane + e * 64 < segs) stats(a)[(size_t)row * segs + lane + e * 64].z = e ? w1 : w0;
+    }
     if (a.u) {
       const double target = target_of(u, z), b0 = wave_before(w0), b1 = z0 + wave_before(w1);
       const uint64_t in0 = __ballot(w0 > 0.0 && b0 <= target), in1 = __ballot(w1 > 0.0 && b1 <= target);
@@ -1181,6 +1186,10 @@ __global__ __launch_bounds__(BS, BS / 256) void row_kernel(const SampleArgs a) {
         }
       }
     }
+  }
+  if (!a.u && !(arg != INT_MAX && st.kind != ONE && top > -INF)) {  // the first alone
+    __syncthreads();
+    for (int s = tid; s < segs; s += BS) stats(a)[(size_t)row * segs + s].z = arg != INT_MAX && s == arg / SEG ? 1.0 : 0.0;
   }
   if (wave == writer && lane == 0) {
     if (a.ids) a.ids[row] = d.id;
@@ -1281,7 +1290,9 @@ template <int NW, class F> __device__ __forceinline__ void rest_steps(const Rest
   }
 }
 
-// One workgroup per (sequence, segment of the vocabulary): the segment's rest, and by the first one the accepted slots.
+// One workgroup per (sequence, segment of the vocabulary): the segment's rest, and by the first one the accepted slots.  Without
+// a draft distribution at that place the rest is the target's own but for one token, and a segment without it weighs what the row kernel
+// found (read again, 128 rows of 152064 took 38 us).
 __global__ __launch_bounds__(256) void rest_sum_kernel(const SampleAcceptArgs a, int segs) {
   __shared__ int redi[4];
   __shared__ double redd[4];
@@ -1289,8 +1300,12 @@ __global__ __launch_bounds__(256) void rest_sum_kernel(const SampleAcceptArgs a,
   const int n = accepted(a, b, redi);
   const Rest r = rest_of(a, b, n);
   double sum = 0.0;
-  rest_steps<4>(r, seg * SEG, a.V, [&](int, double s) { sum += s; });
-  sum = block_reduce<256>(sum, redd, [](double x, double y) { return x + y; });
+  if (!r.q && (r.dead < 0 || r.dead / SEG != seg)) {
+    sum = static_cast<const SegStat *>(a.stat)[((size_t)b * (a.k + 1) + n) * segs + seg].z * r.p_z;
+  } else {
+    rest_steps<4>(r, seg * SEG, a.V, [&](int, double s) { sum += s; });
+    sum = block_reduce<256>(sum, redd, [](double x, double y) { return x + y; });
+  }
   if (threadIdx.x == 0) {
     a.part[(size_t)b * segs + seg] = sum;
     if (seg == 0) a.n[b] = n;

@@ -281,6 +281,7 @@ struct SampleAcceptArgs {
   const int32_t *draft;       // [B][k]
   const float *target;        // [B][k+1][V]
   const SampleDist *dist;     // [B][k+1]
+  const void *stat;           // [B][k+1][segments]: summaries, with the kept weights
   const float *draft_logits;  // [B][k][V] or null
   const SampleDist *draft_dist;
   const float *u_accept, *u_sample;

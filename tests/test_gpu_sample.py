@@ -187,7 +187,7 @@ def run_accept(eng, k, target, dl, draft, ua, us, ud, per, sampled):
 
 
 @pytest.mark.parametrize("sampled", [True, False])
-@pytest.mark.parametrize("B,k,V", [(1, 0, 5), (1, 1, 1), (3, 4, 2), (14, 4, 777), (14, 7, 8193), (28, 2, 20001), (1, 127, 64)])
+@pytest.mark.parametrize("B,k,V", [(1, 0, 5), (1, 1, 1), (3, 4, 2), (14, 4, 777), (14, 7, 8193), (28, 2, 20001), (1, 127, 64), (14, 3, 70001)])
 def test_acceptance(B, k, V, sampled):
     eng = engine(B, max(k, 1))
     per = [MIX[b % len(MIX)] for b in range(B)]

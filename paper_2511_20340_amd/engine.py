@@ -247,13 +247,15 @@ class Engine:
         """From now on every sequence of the steps continues the first `length` (default: all) positions that `one`, an engine
         of the same shapes with B = 1, has in its caches.  start: begin behind them, no keys of their own yet, with one's pending
         token and newest hooked row.  one=None: no prefix any more."""
-        self._prefix = None
         if one is None:
             sfb.check(self.lib.sf_set_prefix(self.ctx, None), "sf_set_prefix", self.ctx)
+            self._prefix = None
             return
         shape = lambda e: {n: v for n, v in e.cfg.items() if n != "vocab"}  # noqa: E731
         if one.B != 1 or shape(one) != shape(self) or one.dev != self.dev:
             raise ValueError("sf_set_prefix: the prefix comes from an engine of the same shapes and device with B = 1")
+        if one.tk.data_ptr() == self.tk.data_ptr() or one._prefix is not None:
+            raise ValueError("sf_set_prefix: the prefix's engine has caches of its own, and no prefix in front of them")
         held = int(one.kv_len[0].item())
         length = held if length is None else int(length)
         if not 1 <= length <= held:
@@ -272,7 +274,8 @@ class Engine:
                 self.n_new.fill_(1)
                 self.pending.copy_(one.pending.expand(self.B))
                 self.hooks[:, 0] = one.hooks[0, newest]
-                self.len_upper = 0
+                if not self._pinned:
+                    self.len_upper = 0
 
     # ---- state helpers (plumbing) ------------------------------------------------------------
     def set_state(self, kv_len=None, pending=None, n_new=None):

@@ -265,3 +265,25 @@ def test_set_prefix_refuses_and_ends():
     assert torch.equal(eng.prefill(prompts), ref.prefill(prompts))
     a, b = (x.sf_verify_step(2, torch.ones(2, 2, dtype=torch.int32, device="cuda"))[0] for x in (eng, ref))
     assert torch.equal(a, b)
+
+
+def test_a_refused_prefix_leaves_the_one_before():
+    """What is refused changes nothing; an engine's own caches and a prefix behind a prefix are; a pinned bound stays pinned."""
+    shape, std = SHAPES["tiny"]
+    _, eng, one = engines(shape, std, 1, 64, 2, 5, synth.prompts([20], shape.vocab, 5)[0])
+    kept, draft = eng._prefix, torch.ones(1, 2, dtype=torch.int32, device="cuda")
+    want = eng.sf_verify_step(2, draft)[0].clone()
+    third = Engine(shape.cfg(), 1, 64, 2)
+    for bad in (eng, Engine(shape.cfg(), 1, 64, 2, share_caches=eng)):
+        with pytest.raises(ValueError):
+            eng.sf_set_prefix(bad, start=False)
+    with pytest.raises(ValueError):
+        third.sf_set_prefix(eng)
+    with pytest.raises(ValueError):
+        eng.sf_set_prefix(one, length=21)
+    assert eng._prefix is kept and torch.equal(eng.sf_verify_step(2, draft)[0], want)
+    eng.pin_len_upper()
+    bound = eng.len_upper
+    eng.sf_set_prefix(one)
+    assert eng.len_upper == bound and torch.equal(eng.sf_verify_step(2, draft)[0], want)
+    assert eng.sf_check_state() == 0

@@ -80,6 +80,8 @@ def test_set_prefix_validates():
     assert L.sf_draft_step(ctx, C.byref(s), 4, sfb.SF_MASK_BIDIR, 0, FAKE, None, None) == sfb.SF_ECAPACITY
     assert call(dk=None, dv=None) == sfb.SF_OK
     assert L.sf_draft_step(ctx, C.byref(s), 4, sfb.SF_MASK_BIDIR, 0, FAKE, None, None) == sfb.SF_ESTATE
+    for last in (0, 1):                                              # before the block's verify and commit
+        assert L.sf_prefill_step(ctx, C.byref(s), 4, FAKE, FAKE, 4, FAKE, 0, 4, 2, last, FAKE, FAKE, FAKE, FAKE, None) == sfb.SF_ESTATE
     assert call() == sfb.SF_OK
     two_stage = sfb.SF_MASK_BIDIR | sfb.SF_DRAFT_TWO_STAGE
     assert L.sf_draft_step(ctx, C.byref(s), 4, two_stage, 0, FAKE, None, None) == sfb.SF_EUNSUPPORTED

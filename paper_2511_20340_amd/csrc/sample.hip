@@ -677,19 +677,18 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
             const int rel = (int)fminf(first - grid_place(v, gf), (float)(BINS - 1));
             atomicAdd((unsigned long long *)&hist[wave][rel], 1ull << BIN_COUNT);
           }
-        if (bound > -INF) limit = out.bucket - bucket_of(bound, gf);
+        limit = sample_whole_bins(bound > -INF, out.bucket, bucket_of(bound, gf));
       }
       __syncthreads();
       static_assert(BINS == 256, "a bin for each thread");
       const uint64_t bin = hist[0][tid] + hist[1][tid] + hist[2][tid] + hist[3][tid];
       if (mass) bins(a)[cell * BINS + tid] = bin;
-      // How deep the list goes: as far as it has room; with a count, until the segment alone has so many; with a least
+      // How deep the list goes (sample_takes): as far as it has room; with a count, until the segment alone has so many; with a least
       // weight (where no share of a count's weight hangs on what lies below), until below it even against this segment's largest;
       // with a share, until it has 64 and what lies below is a quarter of what the share leaves out.
       int total;
       const int cnt = (int)(bin >> BIN_COUNT), upto = cnt + block_before<256>(cnt, redi, total);
-      bool take = upto <= ROOM && tid < limit;
-      if (st.k != INT_MAX) take = take && upto - cnt < st.k;
+      bool take = sample_takes(tid, cnt, upto, limit, st.k);
       if (st.m > 0.f && !(st.k != INT_MAX && st.p < 1.f))
         take = take && (double)(out.bucket - tid + 1) >= ((double)top + (double)st.t * log((double)st.m)) * g - 1.0;
       if (mass) {
@@ -720,14 +719,17 @@ __global__ __launch_bounds__(256) void segment_kernel(const SampleArgs a) {
           for (int e = 0; e < 4; ++e) {
             if (m[e] >> lane & 1) {
               const int p = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m[e] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m[e], 0));
-              list_l(a)[cell * ROOM + p] = l[j][e];
-              list_i(a)[cell * ROOM + p] = seg * SEG + (j * 256 + tid) * 4 + e;
+              if (p < ROOM) {
+                list_l(a)[cell * ROOM + p] = l[j][e];
+                list_i(a)[cell * ROOM + p] = seg * SEG + (j * 256 + tid) * 4 + e;
+              }
             }
             at += __popcll(m[e]);
           }
         }
         __syncthreads();
         out.n = n_list;
+        if (n_list > ROOM) { out.n = 0; out.cut = INT_MAX; }  // not by the counts; what lies behind the list does not hang on them
       }
     }
   }

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 #include "../../include/specformer.h"
+#include "sample_rules.h"
 
 namespace sf {
 
@@ -250,7 +251,7 @@ hipError_t launch_accept(const AcceptArgs &a, hipStream_t s);
 constexpr int SAMPLE_MAX_VOCAB = 1 << 20, SAMPLE_MAX_ROWS = 1 << 20;
 constexpr int SAMPLE_SEG = 8192;  // tokens of a row that one workgroup of the first launch holds in registers
 // of every (row, segment) in the workspace: its summary, a histogram of 64-bit bins, room for tokens (logit and index)
-constexpr int SAMPLE_BINS = 256, SAMPLE_ROOM = 512, SAMPLE_STAT_BYTES = 32;
+constexpr int SAMPLE_STAT_BYTES = 32;
 constexpr size_t SAMPLE_CELL_BYTES = SAMPLE_STAT_BYTES + SAMPLE_BINS * 8 + SAMPLE_ROOM * 8;
 // What is kept of a row: the tokens with l > thr, or l == thr and an index <= last; their weights exp((l - top) / temp) sum
 // up to z.  id, prob: the token drawn.

@@ -150,7 +150,8 @@ sf_status sf_bind(sf_ctx *ctx, const sf_target_weights *target, const sf_draft_w
  * all dev, 16-byte aligned, read only, borrowed until the next sf_set_prefix.  workspace: dev, 256-byte aligned,
  * sf_prefix_workspace_bytes of the largest batch, block and capacity (0 in SF_F32 mode: NULL); the steps' order on one stream
  * covers it as it does the state's.  A sequence that starts at kv_len 0 takes n_new = 1 and as hooks row the prefix's newest.
- * SF_DRAFT_TWO_STAGE with a prefix is SF_EUNSUPPORTED.  prefix NULL: none any more. */
+ * SF_DRAFT_TWO_STAGE with a prefix is SF_EUNSUPPORTED.  prefix NULL: none any more.  A block verified before the call can not be
+ * committed after it (SF_ESTATE); a call that is refused changes nothing. */
 typedef struct {
   int32_t len, cap;
   const void *tk, *tv, *dk, *dv;

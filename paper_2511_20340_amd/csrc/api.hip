@@ -618,14 +618,20 @@ size_t sf_prefix_workspace_bytes(const sf_ctx *c, int32_t B, int32_t k, int32_t 
 
 sf_status sf_set_prefix(sf_ctx *c, const sf_prefix *p) {
   if (!c) return SF_EINVAL;
-  if (!p) { c->prefix = sf_prefix{}; return SF_OK; }
+  // a block verified over the keys in front until now is not this prefix's to commit
+  auto set = [&](const sf_prefix &now) {
+    c->prefix = now;
+    c->verified_state = nullptr;
+    c->verified_k = -1;
+    return SF_OK;
+  };
+  if (!p) return set(sf_prefix{});
   if (p->len < 1 || p->cap < TK || p->cap % TK || !p->tk || !p->tv || !p->dk != !p->dv) return SF_EINVAL;
   if (((uintptr_t)p->tk | (uintptr_t)p->tv | (uintptr_t)p->dk | (uintptr_t)p->dv) % 16) return SF_EINVAL;
   if (p->workspace ? ((uintptr_t)p->workspace) % ALIGN != 0 : c->tc.dtype == SF_BF16) return SF_EINVAL;
   if (p->len > p->cap) return SF_ECAPACITY;
   if ((size_t)p->cap * c->tc.head_dim * esize(c->tc.dtype) >= (1ull << 32)) return SF_EUNSUPPORTED;
-  c->prefix = *p;
-  return SF_OK;
+  return set(*p);
 }
 
 sf_status sf_verify_step(sf_ctx *c, const sf_state *st, int32_t k, const int32_t *draft, int32_t len_upper,

@@ -139,9 +139,11 @@ __device__ __forceinline__ void prefix_rows(const int id, char *smem, const bf16
       for (int v = 0; v < 16; ++v) mx = fmaxf(mx, sc[t][v]);
     mx = fmaxf(mx, __shfl_xor(mx, 32)) * scale_log2e;
     // The maximum follows the scores in strides: as long as they stay below 2^8 times its weight, sums and products in float
-    // lose nothing by an old one, and the accumulators need not be scaled.
-    if (__any(mx > m_run + 8.f)) {
-      const float m_new = fmaxf(m_run, mx);
+    // lose nothing by an old one, and the accumulators need not be scaled.  A row goes by its own scores, which decide how its p are
+    // rounded; the wave's other rows (of other sequences) only by whether the branch is taken.
+    const bool rises = mx > m_run + 8.f;
+    if (__any(rises)) {
+      const float m_new = rises ? mx : m_run;
       const float alpha = __builtin_amdgcn_exp2f(m_run - (m_new == NEG_INF ? 0.f : m_new));
       m_run = m_new;
       l_run *= alpha;

@@ -272,20 +272,27 @@ struct Prefix {
   int len, cap;
   void *ws;
 };
+// What the chunks of the keys are cut for.  An operation: its own rows and keys.  A step: rows of the largest block and the caches'
+// capacity, so that a row's sums have the same order in every block length and at every length bound.  Blocks of the largest length
+// keep their time; a step of one row a sequence in a context for five (128 sequences of 40 / 8 heads of 128, 8192 shared keys): 84 + 7 us
+// a layer, cut for itself 67 + 11.
+struct PrefixCut {
+  int B, n_q, keys;
+};
 // floats of the partials: the prefix's rows x chunks, then the own ones (a partial of every chunk), hd + 2 each
-size_t prefix_ws_rows(const sf_model_cfg &m, int B, int n_q, int prefix_len, int len_upper, size_t *own) {
-  const PrefixPlan p = prefix_plan(B, n_q, m.n_q_heads, m.n_kv_heads, prefix_len);
+size_t prefix_ws_rows(const sf_model_cfg &m, int B, int n_q, int prefix_len, int len_upper, const PrefixCut &cut, size_t *own) {
+  const PrefixPlan p = prefix_plan(B, n_q, m.n_q_heads, m.n_kv_heads, prefix_len, cut.B * cut.n_q);
   const size_t n_rt = (m.n_q_heads / m.n_kv_heads * n_q + 31) / 32, n_tiles = ((size_t)len_upper + n_q + TK - 1) / TK;
   *own = (size_t)B * m.n_kv_heads * ((n_tiles + 15) / 16) * n_rt * 32;  // chunks have 16 tiles at least
   return (size_t)m.n_kv_heads * p.n_chunks * p.rows;
 }
-size_t prefix_ws_bytes(const sf_model_cfg &m, int B, int n_q, int prefix_len, int len_upper) {
+size_t prefix_ws_bytes(const sf_model_cfg &m, int B, int n_q, int prefix_len, int len_upper, const PrefixCut &cut) {
   if (m.dtype != SF_BF16) return 0;
-  size_t own, pre = prefix_ws_rows(m, B, n_q, prefix_len, len_upper, &own);
+  size_t own, pre = prefix_ws_rows(m, B, n_q, prefix_len, len_upper, cut, &own);
   return up((pre + own) * (m.head_dim + 2) * sizeof(float));
 }
-void prefix_attention(Run &r, const sf_model_cfg &m, const Prefix &pre, const void *q, const void *kc, const void *vc,
-                      const int32_t *kv_len, void *out, int B, int n_q, int cap, int mode, int len_upper,
+void prefix_attention(Run &r, const sf_model_cfg &m, const Prefix &pre, const PrefixCut &cut, const void *q, const void *kc,
+                      const void *vc, const int32_t *kv_len, void *out, int B, int n_q, int cap, int mode, int len_upper,
                       const void *qkv = nullptr, const float2 *table = nullptr, const int32_t *order = nullptr,
                       const int32_t *slots = nullptr) {
   if (r.st != SF_OK) return;
@@ -295,12 +302,12 @@ void prefix_attention(Run &r, const sf_model_cfg &m, const Prefix &pre, const vo
   a.B = B; a.n_q = n_q; a.Hq = m.n_q_heads; a.Hkv = m.n_kv_heads; a.hd = m.head_dim; a.cap = cap; a.mode = mode;
   p.pk = pre.k; p.pv = pre.v; p.len = pre.len; p.cap = pre.cap;
   if (m.dtype != SF_BF16) { LAUNCH(K_ATTN, launch_prefix_f32(p, r.s)); return; }
-  const PrefixPlan pl = prefix_plan(B, n_q, a.Hq, a.Hkv, pre.len);
+  const PrefixPlan pl = prefix_plan(B, n_q, a.Hq, a.Hkv, pre.len, cut.B * cut.n_q);
   p.n_chunks = pl.n_chunks; p.chunk_tiles = pl.chunk_tiles; p.rows = pl.rows;
-  const int n_rt = (a.Hq / a.Hkv * n_q + 31) / 32;
-  a.chunk_tiles = r.c->tune_chunk > 0 ? r.c->tune_chunk : attn_chunk_tiles(B * a.Hkv * n_rt, len_upper + n_q);
+  const int n_rt = (a.Hq / a.Hkv * cut.n_q + 31) / 32;
+  a.chunk_tiles = r.c->tune_chunk > 0 ? r.c->tune_chunk : attn_chunk_tiles(cut.B * a.Hkv * n_rt, cut.keys);
   a.n_chunks = ((len_upper + n_q + TK - 1) / TK + a.chunk_tiles - 1) / a.chunk_tiles;
-  size_t own, rows = prefix_ws_rows(m, B, n_q, pre.len, len_upper, &own);
+  size_t own, rows = prefix_ws_rows(m, B, n_q, pre.len, len_upper, cut, &own);
   p.part_o = (float *)pre.ws; a.part_o = p.part_o + rows * a.hd;
   p.part_ml = a.part_o + own * a.hd; a.part_ml = p.part_ml + rows * 2;
   LAUNCH(K_ATTN, launch_prefix_bf16(p, r.s));
@@ -312,11 +319,12 @@ size_t kv_layer_bytes(const sf_model_cfg &m, int B, int cap) {
 }
 
 // a layer's attention of a pass: over the context's shared prefix, if there is one.  which: 0 target layer `layer`, 1 draft
-sf_status check_prefix(const sf_ctx *c, int which, int B, int n_q, int len_upper) {
+PrefixCut step_cut(const sf_ctx *c, int B, int cap) { return {B, c->max_k + 1, cap}; }
+sf_status check_prefix(const sf_ctx *c, int which, int B, int n_q, int cap, int len_upper) {
   const sf_prefix &p = c->prefix;
   if (p.len == 0) return SF_OK;
   if (which == 1 && (!p.dk || !p.dv)) return SF_ESTATE;
-  return p.workspace_bytes < prefix_ws_bytes(c->tc, B, n_q, p.len, len_upper) ? SF_ECAPACITY : SF_OK;
+  return p.workspace_bytes < prefix_ws_bytes(c->tc, B, n_q, p.len, len_upper, step_cut(c, B, cap)) ? SF_ECAPACITY : SF_OK;
 }
 void pass_attention(Run &r, const sf_model_cfg &m, int which, int layer, const void *q, const void *kc, const void *vc,
                     const int32_t *kv_len, void *out, float *part_o, float *part_ml, int B, int n_q, int cap, int mode,
@@ -328,7 +336,7 @@ void pass_attention(Run &r, const sf_model_cfg &m, int which, int layer, const v
   }
   const size_t at = (size_t)layer * m.n_kv_heads * p.cap * m.head_dim * esize(m.dtype);
   const char *pk = (const char *)(which == 0 ? p.tk : p.dk) + at, *pv = (const char *)(which == 0 ? p.tv : p.dv) + at;
-  prefix_attention(r, m, {pk, pv, p.len, p.cap, p.workspace}, q, kc, vc, kv_len, out, B, n_q, cap, mode, len_upper, qkv, table,
+  prefix_attention(r, m, {pk, pv, p.len, p.cap, p.workspace}, step_cut(r.c, B, cap), q, kc, vc, kv_len, out, B, n_q, cap, mode, len_upper, qkv, table,
                    order, slots);
 }
 
@@ -362,7 +370,7 @@ sf_status verify_pass(sf_ctx *c, const sf_state *st, int32_t k, const int32_t *d
   const sf_model_cfg &m = c->tc;
   const int B = sub.n, q = k + 1, M = B * q, cap = st->cap, qm = c->max_k + 1;
   if ((long)len_upper + q > cap) return SF_ECAPACITY;
-  if ((v = check_attn_shape(m, q)) != SF_OK || (v = check_prefix(c, 0, B, q, len_upper)) != SF_OK) return v;
+  if ((v = check_attn_shape(m, q)) != SF_OK || (v = check_prefix(c, 0, B, q, cap, len_upper)) != SF_OK) return v;
   const Arena A = plan(c, st->B, k, cap);
   char *ws = (char *)st->workspace;
   float *h = (float *)(ws + A.h);                                    // the residual stream
@@ -436,7 +444,7 @@ sf_status draft_pass(sf_ctx *c, const sf_state *st, int32_t k, int32_t mask, int
   const sf_model_cfg &m = c->dc;
   const int B = sub.n, cap = st->cap, qm = c->max_k + 1, Mh = B * qm, Ms = B * k;
   if ((long)len_upper + k > cap) return SF_ECAPACITY;
-  if ((v = check_attn_shape(m, k)) != SF_OK || (v = check_prefix(c, 1, B, k, len_upper)) != SF_OK) return v;
+  if ((v = check_attn_shape(m, k)) != SF_OK || (v = check_prefix(c, 1, B, k, cap, len_upper)) != SF_OK) return v;
   // a sequence without a key of its own has its newest row in the prefix, which the two-stage context attention does not look for
   if (two_stage && c->prefix.len > 0) return SF_EUNSUPPORTED;
   const sf_draft_weights &w = c->dw;
@@ -655,7 +663,7 @@ sf_status sf_prefill_step(sf_ctx *c, const sf_state *st, int32_t k, const int32_
   if (n_seq < 1 || n_seq > st->B || !slots || !block_len || !target_ids || !accept_len || !out_tokens) return SF_EINVAL;
   if (k_draft < 0 || k_draft > c->max_k || (k_draft > 0 && !draft_tokens) || len_after < 0) return SF_EINVAL;
   if (k_draft > k && (v = check_state(c, st, k_draft, true)) != SF_OK) return v;  // room for the draft too, before the commit
-  if (k_draft > 0 && (v = check_prefix(c, 1, n_seq, k_draft, last ? len_after : 0)) != SF_OK) return v;
+  if (k_draft > 0 && (v = check_prefix(c, 1, n_seq, k_draft, st->cap, last ? len_after : 0)) != SF_OK) return v;
   if (last && (long)len_after + k_draft > st->cap) return SF_ECAPACITY;
   const Subset sub{n_seq, slots, last != 0};
   if ((v = verify_pass(c, st, k, tokens, len_upper, nullptr, target_ids, stream, sub)) != SF_OK) return v;
@@ -759,7 +767,7 @@ sf_status sf_op_attention(const sf_ctx *c, const void *q, const void *kc, const 
 size_t sf_prefix_attention_workspace_bytes(const sf_ctx *c, int32_t B, int32_t n_q, int32_t prefix_len, int32_t len_upper) {
   if (!c || B < 1 || n_q < 1 || prefix_len < 0 || len_upper < 0 || (long)B * n_q > SF_PREFIX_MAX_ROWS) return 0;
   if (prefix_len == 0) return sf_attention_workspace_bytes(c, B, n_q, len_upper);
-  return prefix_ws_bytes(c->tc, B, n_q, prefix_len, len_upper);
+  return prefix_ws_bytes(c->tc, B, n_q, prefix_len, len_upper, {B, n_q, len_upper + n_q});
 }
 
 sf_status sf_op_prefix_attention(const sf_ctx *c, const void *q, const void *pk, const void *pv, int32_t prefix_len,
@@ -781,7 +789,7 @@ sf_status sf_op_prefix_attention(const sf_ctx *c, const void *q, const void *pk,
   if (prefix_len == 0)
     return sf_op_attention(c, q, kc, vc, kv_len, B, n_q, cap, mask, len_upper, out, workspace, workspace_bytes, stream);
   Run r{c, (hipStream_t)stream};
-  prefix_attention(r, m, {pk, pv, prefix_len, prefix_cap, workspace}, q, kc, vc, kv_len, out, B, n_q, cap, mask, len_upper);
+  prefix_attention(r, m, {pk, pv, prefix_len, prefix_cap, workspace}, {B, n_q, len_upper + n_q}, q, kc, vc, kv_len, out, B, n_q, cap, mask, len_upper);
   return r.st;
 }
 

@@ -370,11 +370,11 @@ template <int HD> hipError_t pick_prefix(const PrefixKernelArgs &a, bool fuse, h
 
 }  // namespace
 
-PrefixPlan prefix_plan(int B, int n_q, int Hq, int Hkv, int len) {
-  const int R = B * n_q * (Hq / Hkv), n_tiles = (len + TK - 1) / TK;
+PrefixPlan prefix_plan(int B, int n_q, int Hq, int Hkv, int len, int plan_rows) {
+  const int G = Hq / Hkv, n_tiles = (len + TK - 1) / TK;
   PrefixPlan p;
-  const int row_tiles = (R + 127) / 128;
-  p.rows = row_tiles * 128;
+  p.rows = (B * n_q * G + 127) / 128 * 128;
+  const int row_tiles = (plan_rows * G + 127) / 128;
   // As many workgroups as the chip holds at once (two to a compute unit), not more: a chunk more costs its partials.  128 x 5
   // rows, 8192 keys, in 1, 2, 3, 4 chunks: 173, 157, 163, 161 us with the join; 37 x 4 rows, 1500 keys: 38, 27, 25, 25, in 5
   // and 6 26 and 26.  Below 12 tiles to a chunk nothing is gained unless the rows are one tile and all is latency.

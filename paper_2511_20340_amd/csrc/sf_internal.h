@@ -110,7 +110,8 @@ struct PrefixPlan {
   int rows;  // (b, block row, query head of the kv head), padded to whole workgroups
   int chunk_tiles, n_chunks;
 };
-PrefixPlan prefix_plan(int B, int n_q, int Hq, int Hkv, int len);
+// plan_rows: (b, block row) pairs that the chunks are cut for, B * n_q or more of them
+PrefixPlan prefix_plan(int B, int n_q, int Hq, int Hkv, int len, int plan_rows);
 // rows x chunks of the plan of any batch up to B and block up to n_q
 size_t prefix_rows_bound(int B, int n_q, int Hq, int Hkv);
 hipError_t launch_prefix_bf16(const PrefixArgs &a, hipStream_t s);     // partials of the prefix and of the own keys

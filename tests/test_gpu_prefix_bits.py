@@ -1,9 +1,13 @@
-"""What a row over a shared prefix does not depend on, to the last bit: the scores of the rows beside it."""
+"""What a row over a shared prefix does not depend on, to the last bit: the scores of the rows beside it, the length of the block
+that it is verified in."""
 import pytest
 import torch
 
+import synth
 from paper_2511_20340_amd import binding as sfb
+from paper_2511_20340_amd import engine as E
 
+from test_gpu_e2e import SLICES
 from test_gpu_prefix_attention import call, load, make
 
 pytestmark = pytest.mark.gpu
@@ -26,3 +30,47 @@ def test_a_row_does_not_hang_on_its_neighbours(heads, B, n_q):
             other[b] = q[b]
             got = call(eng, one, other, P, lens, n_q, sfb.SF_MASK_CAUSAL)[b]
             assert torch.equal(got, want), (b, scale)
+
+
+def engines(shape, B, cap, k, seed, P, n=1):
+    tw, dw = synth.target_weights(shape, seed, 0.05), synth.draft_weights(shape, k, seed, 0.05)
+    one = E.Engine(shape.cfg(), 1, -(-(P + 8) // 32) * 32, 3)
+    one.bind(tw, dw)
+    one.prefill(synth.prompts([P], shape.vocab, seed), block=64)
+    out = [E.Engine(shape.cfg(), B, cap, k) for _ in range(n)]
+    for e in out:
+        e.bind(tw, dw)
+        e.sf_set_prefix(one)
+    return one, out
+
+
+@pytest.mark.parametrize("name,B,P,tail", [("8b-slice", 12, 1000, 10), ("1b-slice", 12, 1500, 40), ("14b-slice", 5, 900, 600)])
+def test_one_engine_switching_between_plain_and_speculative_steps(name, B, P, tail):
+    """Plain greedy steps (k = 0) and a verified block (k = 4) of one engine give the same logits for the same rows: over the
+    prefix alone and over tails of their own, short and of several chunks."""
+    m, k, seed = SLICES[name], 4, 23
+    cap = -(-(tail + 4 * (k + 1)) // 32) * 32
+    _, (eng,) = engines(m, B, cap, k, seed, P)
+    none = torch.zeros(B, 0, dtype=torch.int32, device="cuda")
+    for start in ("prefix", "tails"):
+        if start == "tails":
+            eng.prefill(synth.prompts([max(1, tail - 3 * b) for b in range(B)], m.vocab, seed + 1), block=16)
+        else:
+            eng.pending.copy_(torch.arange(B, device="cuda") * 17 + 3)    # sequences that differ
+        snap = {n: getattr(eng, n).clone() for n in ("kv_len", "pending", "n_new", "cu_new", "hooks")}
+        len0 = eng.len_upper
+        toks, rows = [eng.pending.clone()], []
+        for _ in range(k + 1):
+            lg, ids = eng.sf_verify_step(0, none)
+            rows.append(lg[:, 0].clone())
+            _, out = eng.sf_accept_commit(0, none, ids)
+            toks.append(out[:, 0].clone())
+        for n, t in snap.items():
+            getattr(eng, n).copy_(t)
+        eng.len_upper = len0
+        draft = torch.stack(toks[1:k + 1], 1).contiguous()
+        lg, ids = eng.sf_verify_step(k, draft)
+        for i in range(k + 1):
+            assert torch.equal(lg[:, i], rows[i]), (start, i)
+        acc, _ = eng.sf_accept_commit(k, draft, ids)
+        assert acc.cpu().tolist() == [k + 1] * B, start

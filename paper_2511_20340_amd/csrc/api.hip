@@ -272,8 +272,9 @@ struct Prefix {
   int len, cap;
   void *ws;
 };
-// What the chunks of the keys are cut for.  An operation: its own rows and keys.  A step: rows of the largest block and the caches'
-// capacity, so that a row's sums have the same order in every block length and at every length bound.  Blocks of the largest length
+// What the chunks of the keys are cut for.  An operation: its own rows and keys.  A step: rows of the largest block of the whole batch
+// and the caches' capacity, so that a row's sums have the same order in every block length, at every length bound and in a part of
+// the batch.  Blocks of the largest length
 // keep their time; a step of one row a sequence in a context for five (128 sequences of 40 / 8 heads of 128, 8192 shared keys): 84 + 7 us
 // a layer, cut for itself 67 + 11.
 struct PrefixCut {
@@ -318,14 +319,14 @@ size_t kv_layer_bytes(const sf_model_cfg &m, int B, int cap) {
   return (size_t)B * m.n_kv_heads * cap * m.head_dim * esize(m.dtype);
 }
 
-// a layer's attention of a pass: over the context's shared prefix, if there is one.  which: 0 target layer `layer`, 1 draft
-PrefixCut step_cut(const sf_ctx *c, int B, int cap) { return {B, c->max_k + 1, cap}; }
-sf_status check_prefix(const sf_ctx *c, int which, int B, int n_q, int cap, int len_upper) {
+PrefixCut step_cut(const sf_ctx *c, int whole_B, int cap) { return {whole_B, c->max_k + 1, cap}; }
+sf_status check_prefix(const sf_ctx *c, int which, const sf_state *st, int B, int n_q, int len_upper) {
   const sf_prefix &p = c->prefix;
   if (p.len == 0) return SF_OK;
   if (which == 1 && (!p.dk || !p.dv)) return SF_ESTATE;
-  return p.workspace_bytes < prefix_ws_bytes(c->tc, B, n_q, p.len, len_upper, step_cut(c, B, cap)) ? SF_ECAPACITY : SF_OK;
+  return p.workspace_bytes < prefix_ws_bytes(c->tc, B, n_q, p.len, len_upper, step_cut(c, st->B, st->cap)) ? SF_ECAPACITY : SF_OK;
 }
+// a layer's attention of a pass: over the context's shared prefix, if there is one.  which: 0 target layer `layer`, 1 draft
 void pass_attention(Run &r, const sf_model_cfg &m, int which, int layer, const void *q, const void *kc, const void *vc,
                     const int32_t *kv_len, void *out, float *part_o, float *part_ml, int B, int n_q, int cap, int mode,
                     int len_upper, const void *qkv, const float2 *table, const int32_t *order, const int32_t *slots, int plan_B) {
@@ -336,8 +337,8 @@ void pass_attention(Run &r, const sf_model_cfg &m, int which, int layer, const v
   }
   const size_t at = (size_t)layer * m.n_kv_heads * p.cap * m.head_dim * esize(m.dtype);
   const char *pk = (const char *)(which == 0 ? p.tk : p.dk) + at, *pv = (const char *)(which == 0 ? p.tv : p.dv) + at;
-  prefix_attention(r, m, {pk, pv, p.len, p.cap, p.workspace}, step_cut(r.c, B, cap), q, kc, vc, kv_len, out, B, n_q, cap, mode, len_upper, qkv, table,
-                   order, slots);
+  prefix_attention(r, m, {pk, pv, p.len, p.cap, p.workspace}, step_cut(r.c, plan_B, cap), q, kc, vc, kv_len, out, B, n_q, cap, mode,
+                   len_upper, qkv, table, order, slots);
 }
 
 // The sequences a pass runs over: rows and state arrays 0..n-1, whose caches are those of sequence slots[j] (null: j).
@@ -370,7 +371,7 @@ sf_status verify_pass(sf_ctx *c, const sf_state *st, int32_t k, const int32_t *d
   const sf_model_cfg &m = c->tc;
   const int B = sub.n, q = k + 1, M = B * q, cap = st->cap, qm = c->max_k + 1;
   if ((long)len_upper + q > cap) return SF_ECAPACITY;
-  if ((v = check_attn_shape(m, q)) != SF_OK || (v = check_prefix(c, 0, B, q, cap, len_upper)) != SF_OK) return v;
+  if ((v = check_attn_shape(m, q)) != SF_OK || (v = check_prefix(c, 0, st, B, q, len_upper)) != SF_OK) return v;
   const Arena A = plan(c, st->B, k, cap);
   char *ws = (char *)st->workspace;
   float *h = (float *)(ws + A.h);                                    // the residual stream
@@ -444,7 +445,7 @@ sf_status draft_pass(sf_ctx *c, const sf_state *st, int32_t k, int32_t mask, int
   const sf_model_cfg &m = c->dc;
   const int B = sub.n, cap = st->cap, qm = c->max_k + 1, Mh = B * qm, Ms = B * k;
   if ((long)len_upper + k > cap) return SF_ECAPACITY;
-  if ((v = check_attn_shape(m, k)) != SF_OK || (v = check_prefix(c, 1, B, k, cap, len_upper)) != SF_OK) return v;
+  if ((v = check_attn_shape(m, k)) != SF_OK || (v = check_prefix(c, 1, st, B, k, len_upper)) != SF_OK) return v;
   // a sequence without a key of its own has its newest row in the prefix, which the two-stage context attention does not look for
   if (two_stage && c->prefix.len > 0) return SF_EUNSUPPORTED;
   const sf_draft_weights &w = c->dw;
@@ -663,7 +664,7 @@ sf_status sf_prefill_step(sf_ctx *c, const sf_state *st, int32_t k, const int32_
   if (n_seq < 1 || n_seq > st->B || !slots || !block_len || !target_ids || !accept_len || !out_tokens) return SF_EINVAL;
   if (k_draft < 0 || k_draft > c->max_k || (k_draft > 0 && !draft_tokens) || len_after < 0) return SF_EINVAL;
   if (k_draft > k && (v = check_state(c, st, k_draft, true)) != SF_OK) return v;  // room for the draft too, before the commit
-  if (k_draft > 0 && (v = check_prefix(c, 1, n_seq, k_draft, st->cap, last ? len_after : 0)) != SF_OK) return v;
+  if (k_draft > 0 && (v = check_prefix(c, 1, st, n_seq, k_draft, last ? len_after : 0)) != SF_OK) return v;
   if (last && (long)len_after + k_draft > st->cap) return SF_ECAPACITY;
   const Subset sub{n_seq, slots, last != 0};
   if ((v = verify_pass(c, st, k, tokens, len_upper, nullptr, target_ids, stream, sub)) != SF_OK) return v;

@@ -1,5 +1,6 @@
 """What a row over a shared prefix does not depend on, to the last bit: the scores of the rows beside it, the length of the block
-that it is verified in."""
+that it is verified in, the part of the batch that runs."""
+import numpy as np
 import pytest
 import torch
 
@@ -74,3 +75,27 @@ def test_one_engine_switching_between_plain_and_speculative_steps(name, B, P, ta
             assert torch.equal(lg[:, i], rows[i]), (start, i)
         acc, _ = eng.sf_accept_commit(k, draft, ids)
         assert acc.cpu().tolist() == [k + 1] * B, start
+
+
+@pytest.mark.parametrize("name,block,lens,P", [("8b-slice", 16, [1, 15, 16, 17, 40, 40, 3, 64], 1500), ("1b-slice", 8, [5, 30, 8, 8, 9], 1500),
+                                               ("14b-slice", 32, [700, 1, 33, 580], 900)])
+def test_packed_prefill_keeps_the_whole_batchs_bits(name, block, lens, P):
+    """Tails prefilled over the prompts that have started leave what running all of them in every block leaves."""
+    m, k, seed, B = SLICES[name], 4, 29, len(lens)
+    cap = -(-(max(lens) + block + k) // 32) * 32
+    one, (eng, ref) = engines(m, B, cap, k, seed, P, n=2)
+    prompts = synth.prompts(lens, m.vocab, seed + 2)
+    first = eng.prefill(prompts, block=block)
+    helper = E.Engine(ref.cfg, B, cap, block - 1, share_caches=ref)
+    helper.bind_shared(ref, with_draft=True)
+    helper.sf_set_prefix(one, start=False)
+    want = E._prefill_blocks(helper, prompts, block, k)
+    torch.cuda.synchronize()
+    assert eng.kv_len.tolist() == lens
+    for which, layers in (("tk", m.n_layers), ("tv", m.n_layers), ("dk", 1), ("dv", 1)):
+        for l in range(layers):
+            a, b = eng.sf_kv_export(which, l), ref.sf_kv_export(which, l)
+            for i in range(B):
+                assert torch.equal(a[i, :, :lens[i]], b[i, :, :lens[i]]), (which, l, i)
+    rows = helper.hooks[torch.arange(B), (helper.n_new.long() - 1).cpu()]
+    assert torch.equal(eng.hooks[:, 0], rows) and torch.equal(first, want)

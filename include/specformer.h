@@ -146,7 +146,8 @@ sf_status sf_bind(sf_ctx *ctx, const sf_target_weights *target, const sf_draft_w
  * computed once, stand in front of every sequence and are read once per layer for all of them.  Positions count from its start:
  * kv_len[b] (and host_len_upper, cap) are a sequence's own keys, its row i sits at position len + kv_len[b] + i.
  *   tk, tv  caches of ONE sequence of capacity cap (multiple of 32), as a state of B = 1 has them after a prefill of the prefix
- *   dk, dv  its draft caches; NULL when sf_draft_step is not called (SF_ESTATE there)
+ *   dk, dv  its draft caches, with the keys of all len positions (a block's are written by the draft step after its commit);
+ *           NULL when sf_draft_step is not called (SF_ESTATE there)
  * all dev, 16-byte aligned, read only, borrowed until the next sf_set_prefix.  workspace: dev, 256-byte aligned,
  * sf_prefix_workspace_bytes of the largest batch, block and capacity (0 in SF_F32 mode: NULL); the steps' order on one stream
  * covers it as it does the state's.  A sequence that starts at kv_len 0 takes n_new = 1 and as hooks row the prefix's newest.

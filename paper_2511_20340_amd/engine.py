@@ -2,6 +2,7 @@
 tensors and hands their pointers to the C ABI.  Method names mirror the C entry points; no step
 of the path is computed here (torch is used for memory, streams and host<->device copies only).
 """
+import collections
 import contextlib
 import ctypes as C
 
@@ -26,6 +27,10 @@ def _stream():
 def _stream_addr():
     """The current stream's handle; with the device's index given, torch finds it in half the time (1.3 us, not 2.7)."""
     return torch.cuda.current_stream(torch.cuda.current_device()).cuda_stream
+
+
+# what the sequences of an engine continue: the engine that holds it, its positions, whether their draft keys are there
+_Prefix = collections.namedtuple("_Prefix", "one length drafted workspace")
 
 
 class Engine:
@@ -79,6 +84,8 @@ class Engine:
         self.len_upper = 0          # host-side upper bound of max_b kv_len[b]
         self._prefix = None
         self._pinned = False
+        self._D = None
+        self._undrafted = 0         # blocks committed since the draft step that last wrote draft keys (2: some are lost)
         self._keep = []
 
     def close(self):
@@ -179,6 +186,8 @@ class Engine:
         out = draft_out if draft_out is not None else torch.empty(self.B, max(k, 0), dtype=torch.int32, device=self.dev)
         sfb.check(self.lib.sf_draft_step(self.ctx, C.byref(self.st), k, mask, self.len_upper, _ptr(out),
                                          _ptr(logits_out), _stream()), "sf_draft_step", self.ctx)
+        if self._undrafted == 1:
+            self._undrafted = 0
         return out
 
     def sf_verify_step(self, k, draft, logits_out=None, ids_out=None, logits=True):
@@ -199,9 +208,14 @@ class Engine:
         sfb.check(self.lib.sf_accept_commit(self.ctx, C.byref(self.st), k, _ptr(draft) if k > 0 else None,
                                             _ptr(target_ids), _ptr(force_len), _ptr(acc), _ptr(out), _stream()),
                   "sf_accept_commit", self.ctx)
+        self._committed(k)
+        return acc, out
+
+    def _committed(self, k):
+        """A block of k + 1 rows was committed: the host's bound, and that its draft keys wait for a draft step."""
+        self._undrafted = min(self._undrafted + 1, 2)
         if not self._pinned:
             self.len_upper = min(self.len_upper + k + 1, self.cap)
-        return acc, out
 
     def sf_check_state(self):
         """-> SF_DEVERR_* bits the device collected since the last check (0 = none); waits for the stream."""
@@ -218,6 +232,7 @@ class Engine:
         sfb.check(self.lib.sf_op_accept(self.ctx, self.B, k, _ptr(draft) if k > 0 else None, _ptr(target_ids),
                                         _ptr(force_len), _ptr(acc), _ptr(out), _ptr(self.kv_len), _ptr(self.pending),
                                         _ptr(self.n_new), _ptr(self.cu_new), _stream()), "sf_op_accept", self.ctx)
+        self._undrafted = min(self._undrafted + 1, 2)
         return acc, out
 
     def sf_tune_linear(self, tile=0, split_k=0):
@@ -246,7 +261,9 @@ class Engine:
     def sf_set_prefix(self, one, length=None, start=True):
         """From now on every sequence of the steps continues the first `length` (default: all) positions that `one`, an engine
         of the same shapes with B = 1, has in its caches.  start: begin behind them, no keys of their own yet, with one's pending
-        token and newest hooked row.  one=None: no prefix any more."""
+        token and newest hooked row.  one=None: no prefix any more.  The draft keys of a block that `one` has committed since its
+        last draft step are written here (by a draft step of one).  Where they can not be, as `one` has no draft weights or has
+        committed several blocks without a draft step, sf_draft_step is refused (SF_ESTATE) behind this prefix."""
         if one is None:
             sfb.check(self.lib.sf_set_prefix(self.ctx, None), "sf_set_prefix", self.ctx)
             self._prefix = None
@@ -263,11 +280,7 @@ class Engine:
         if start and length != held:
             raise ValueError("sf_set_prefix: the newest hooked row is that of the prefix's end; start=False with a part of it")
         with torch.cuda.device(self.dev):
-            nb = self.lib.sf_prefix_workspace_bytes(self.ctx, self.B, self.max_k, self.cap)
-            ws, at = self._workspace(nb)
-            pre = sfb.Prefix(length, one.cap, _addr(one.tk), _addr(one.tv), _addr(one.dk), _addr(one.dv), at if nb else None, nb)
-            sfb.check(self.lib.sf_set_prefix(self.ctx, C.byref(pre)), "sf_set_prefix", self.ctx)
-            self._prefix = (one, length, ws)
+            self._put_prefix(one, length, one._draft_keys(held))
             if start:
                 newest = max(int(one.n_new[0].item()) - 1, 0)
                 self.kv_len.zero_()
@@ -277,11 +290,34 @@ class Engine:
                 if not self._pinned:
                     self.len_upper = 0
 
+    def _draft_keys(self, held):
+        """Whether the draft cache has the keys of all `held` positions, after a draft step for those that only wait for one."""
+        if self._D is not None and self._undrafted == 1 and self.max_k > 0 and held < self.cap:
+            bound, self.len_upper = self.len_upper, held
+            try:
+                self.sf_draft_step(1)
+            finally:
+                self.len_upper = bound
+        return self._D is not None and self._undrafted == 0
+
+    def _put_prefix(self, one, length, drafted):
+        nb = self.lib.sf_prefix_workspace_bytes(self.ctx, self.B, self.max_k, self.cap)
+        ws, at = self._workspace(nb)
+        dk, dv = (one.dk, one.dv) if drafted else (None, None)
+        pre = sfb.Prefix(length, one.cap, _addr(one.tk), _addr(one.tv), _addr(dk), _addr(dv), at if nb else None, nb)
+        sfb.check(self.lib.sf_set_prefix(self.ctx, C.byref(pre)), "sf_set_prefix", self.ctx)
+        self._prefix = _Prefix(one, length, drafted, ws)
+
+    def _drafts(self):
+        """Whether draft steps run here: with draft weights, and not behind a prefix without draft keys."""
+        return self._D is not None and (self._prefix is None or self._prefix.drafted)
+
     # ---- state helpers (plumbing) ------------------------------------------------------------
     def set_state(self, kv_len=None, pending=None, n_new=None):
         if kv_len is not None:
             self.kv_len.copy_(torch.as_tensor(np.asarray(kv_len, dtype=np.int32)))
             self.len_upper = int(np.max(kv_len))
+            self._undrafted = 0     # the caller's word: the caches hold what belongs to these lengths
         if pending is not None:
             self.pending.copy_(torch.as_tensor(np.asarray(pending, dtype=np.int32)))
         if n_new is not None:
@@ -595,8 +631,10 @@ class Engine:
         def call(args, ws):
             return self.lib.sf_op_accept_sampled(self.ctx, self.B, k, V, *args, self.st.kv_len, self.st.pending, self.st.n_new,
                                                  self.st.cu_new, *ws)
-        return self._accept_sampled("sf_op_accept_sampled", call, k, V, draft, target_logits, u_accept, u_sample,
-                                    (temperature, top_k, top_p, min_p), draft_logits, draft_dist, None, None)
+        r = self._accept_sampled("sf_op_accept_sampled", call, k, V, draft, target_logits, u_accept, u_sample,
+                                 (temperature, top_k, top_p, min_p), draft_logits, draft_dist, None, None)
+        self._undrafted = min(self._undrafted + 1, 2)
+        return r
 
     def sf_accept_commit_sampled(self, k, draft, target_logits, u_accept, u_sample, temperature=None, top_k=None, top_p=None,
                                  min_p=None, draft_logits=None, draft_dist=None, accept_out=None, tokens_out=None):
@@ -606,8 +644,7 @@ class Engine:
             return self.lib.sf_accept_commit_sampled(self.ctx, C.byref(self.st), k, *args, *ws)
         r = self._accept_sampled("sf_accept_commit_sampled", call, k, self.V, draft, target_logits, u_accept, u_sample,
                                  (temperature, top_k, top_p, min_p), draft_logits, draft_dist, accept_out, tokens_out)
-        if not self._pinned:
-            self.len_upper = min(self.len_upper + k + 1, self.cap)
+        self._committed(k)
         return r
 
     # ---- prefill: chunked verify with forced acceptance --------------------------------------
@@ -625,7 +662,7 @@ class Engine:
         helper = Engine(self.cfg, self.B, self.cap, q - 1, device=self.dev, share_caches=self)
         helper.bind_shared(self, with_draft=self._D is not None)
         if self._prefix is not None:
-            helper.sf_set_prefix(self._prefix[0], self._prefix[1], start=False)
+            helper._put_prefix(self._prefix.one, self._prefix.length, self._prefix.drafted)
         # row j of the helper is prompt order[j]; its K/V stay in the prompt's own cache slot
         lens = [len(p) for p in prompts]
         if len(lens) == self.B and min(lens) > 0:
@@ -643,6 +680,7 @@ class Engine:
         self.hooks[slots, 0] = rows
         self.n_new[slots] = (helper.n_new > 0).to(torch.int32)
         self.len_upper = helper.len_upper
+        self._undrafted = 2 if helper._undrafted else 0     # of the newest block one row of hooks is left
         torch.cuda.current_stream().synchronize()
         helper.close()
         return self.pending.clone()
@@ -676,12 +714,14 @@ def _prefill_packed(eng, prompts, order, q, k_draft):
     acc, draft = torch.empty(eng.B, **i32), torch.empty(eng.B, k_draft, **i32)
     eng.kv_len.zero_()
     eng.n_new.zero_()
+    drafts = eng._drafts()
+    eng._undrafted = 0 if drafts else 2
     before = 0
     for step in range(total):
         n = int(active[step])
         eng.pending.copy_(d_first[step])
         sfb.check(eng.lib.sf_prefill_step(eng.ctx, C.byref(eng.st), q - 1, _ptr(d_rest[step]), _ptr(d_size[step]), n,
-                                          _ptr(slots), before, int(upper[step]), k_draft if eng._D is not None else 0,
+                                          _ptr(slots), before, int(upper[step]), k_draft if drafts else 0,
                                           int(step == total - 1), _ptr(ids), _ptr(acc), _ptr(out), _ptr(draft), _stream()),
                   "sf_prefill_step", eng.ctx)
         before = int(upper[step])
@@ -715,6 +755,6 @@ def _prefill_blocks(eng, prompts, q, k_draft):
         _, ids = eng.sf_verify_step(k, draft, logits=False)
         eng.sf_accept_commit(k, draft, ids, force_len=fl)
         eng.len_upper = int(done.max())
-        if k_draft > 0 and eng._D is not None:
+        if k_draft > 0 and eng._drafts():
             eng.sf_draft_step(k_draft)
     return eng.pending.clone()

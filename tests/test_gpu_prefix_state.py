@@ -1,4 +1,4 @@
-"""What a context and an engine know about a shared prefix: calls in another order."""
+"""What a context and an engine know about a shared prefix: calls in another order, a prefix whose draft keys are not there."""
 import pytest
 import torch
 
@@ -36,3 +36,75 @@ def test_a_block_verified_over_another_prefix_is_not_committed():
     with pytest.raises(ValueError):
         eng.sf_set_prefix(one, length=0)                     # refused: the block stays
     eng.sf_accept_commit(k, draft, ids)
+
+
+def logits_of_a_draft(eng, k):
+    dl = torch.empty(eng.B, k, eng.V, device="cuda")
+    eng.sf_draft_step(k, logits_out=dl)
+    return dl
+
+
+@pytest.mark.parametrize("name", SHAPES)
+def test_a_prefix_taken_straight_after_a_commit(name):
+    """The rows of the newest block get their draft keys before the prefix stands in front of anyone."""
+    k, seed, B, P = 3, 7, 3, 40
+    shape, tw, dw = weights(name, k, seed)
+    got = []
+    for drafted in (True, False):
+        one, eng = Engine(shape.cfg(), 1, 64, k), Engine(shape.cfg(), B, 64, k)
+        for e in (one, eng):
+            e.bind(tw, dw)
+        one.prefill(synth.prompts([P], shape.vocab, seed))
+        draft = one.sf_draft_step(k)
+        _, ids = one.sf_verify_step(k, draft)
+        one.sf_accept_commit(k, ids[:, :k].contiguous(), ids)             # all of the block
+        assert one.kv_len.tolist() == [P + k + 1]
+        if drafted:
+            one.sf_draft_step(k)
+        eng.sf_set_prefix(one)
+        assert one.kv_len.tolist() == [P + k + 1] and one.n_new.tolist() == [k + 1]
+        got.append(logits_of_a_draft(eng, k))
+    assert torch.equal(got[0], got[1])
+
+
+def prefixes_without_draft_keys(shape, tw, dw, k, seed):
+    prompt = synth.prompts([30], shape.vocab, seed)
+    target_only = Engine(shape.cfg(), 1, 64, k)
+    target_only.bind(tw)
+    target_only.prefill(prompt)
+    plain = Engine(shape.cfg(), 1, 64, 0)                    # prefilled token by token, without a draft step
+    plain.bind(tw, dw)
+    plain.prefill(prompt)
+    behind = Engine(shape.cfg(), 1, 64, k)                   # two blocks committed, none drafted
+    behind.bind(tw, dw)
+    behind.prefill(prompt)
+    none = torch.zeros(1, 0, dtype=torch.int32, device="cuda")
+    for _ in range(2):
+        _, ids = behind.sf_verify_step(0, none)
+        behind.sf_accept_commit(0, none, ids)
+    return {"target only": target_only, "plain decoding": plain, "two blocks behind": behind}
+
+
+@pytest.mark.parametrize("name", SHAPES)
+def test_a_prefix_without_draft_keys(name):
+    """Nothing drafts from keys that were never written: the draft step is refused, the target's steps run, tails are
+    prefilled."""
+    k, seed, B = 2, 9, 2
+    shape, tw, dw = weights(name, k, seed)
+    draft = torch.ones(B, k, dtype=torch.int32, device="cuda")
+    for what, one in prefixes_without_draft_keys(shape, tw, dw, k, seed).items():
+        eng, ref = Engine(shape.cfg(), B, 64, k), Engine(shape.cfg(), B, 64, k)
+        eng.bind(tw, dw)
+        ref.bind(tw)
+        for e in (eng, ref):
+            e.sf_set_prefix(one)
+        with pytest.raises(sfb.SfError) as e:
+            eng.sf_draft_step(k)
+        assert e.value.status == sfb.SF_ESTATE, what
+        a, b = (x.sf_verify_step(k, draft)[0] for x in (eng, ref))
+        assert torch.equal(a, b), what
+        for block in (None, 8):
+            tails = synth.prompts([11, 4], shape.vocab, seed + 1)
+            assert torch.equal(eng.prefill(tails, block=block), ref.prefill(tails, block=block)), what
+            a, b = (x.sf_verify_step(k, draft)[0] for x in (eng, ref))
+            assert torch.equal(a, b), what

@@ -29,8 +29,9 @@ def _stream_addr():
     return torch.cuda.current_stream(torch.cuda.current_device()).cuda_stream
 
 
-# what the sequences of an engine continue: the engine that holds it, its positions, whether their draft keys are there
-_Prefix = collections.namedtuple("_Prefix", "one length drafted workspace")
+# What the sequences of an engine continue: the engine that holds it, its positions, whether their draft keys are there, the
+# pending token and newest hooked row behind them (None: the prefix is a part of what the engine holds).
+_Prefix = collections.namedtuple("_Prefix", "one length drafted start workspace")
 
 
 class Engine:
@@ -280,15 +281,21 @@ class Engine:
         if start and length != held:
             raise ValueError("sf_set_prefix: the newest hooked row is that of the prefix's end; start=False with a part of it")
         with torch.cuda.device(self.dev):
-            self._put_prefix(one, length, one._draft_keys(held))
+            newest = max(int(one.n_new[0].item()) - 1, 0)
+            behind = (one.pending.clone(), one.hooks[0, newest].clone()) if length == held else None
+            self._put_prefix(one, length, one._draft_keys(held), behind)
             if start:
-                newest = max(int(one.n_new[0].item()) - 1, 0)
                 self.kv_len.zero_()
-                self.n_new.fill_(1)
-                self.pending.copy_(one.pending.expand(self.B))
-                self.hooks[:, 0] = one.hooks[0, newest]
+                self._start_behind_prefix(slice(None))
+                self._undrafted = 0
                 if not self._pinned:
                     self.len_upper = 0
+
+    def _start_behind_prefix(self, rows):
+        pending, hooked = self._prefix.start
+        self.pending[rows] = pending
+        self.n_new[rows] = 1
+        self.hooks[rows, 0] = hooked
 
     def _draft_keys(self, held):
         """Whether the draft cache has the keys of all `held` positions, after a draft step for those that only wait for one."""
@@ -300,13 +307,13 @@ class Engine:
                 self.len_upper = bound
         return self._D is not None and self._undrafted == 0
 
-    def _put_prefix(self, one, length, drafted):
+    def _put_prefix(self, one, length, drafted, start):
         nb = self.lib.sf_prefix_workspace_bytes(self.ctx, self.B, self.max_k, self.cap)
         ws, at = self._workspace(nb)
         dk, dv = (one.dk, one.dv) if drafted else (None, None)
         pre = sfb.Prefix(length, one.cap, _addr(one.tk), _addr(one.tv), _addr(dk), _addr(dv), at if nb else None, nb)
         sfb.check(self.lib.sf_set_prefix(self.ctx, C.byref(pre)), "sf_set_prefix", self.ctx)
-        self._prefix = _Prefix(one, length, drafted, ws)
+        self._prefix = _Prefix(one, length, drafted, start, ws)
 
     def _drafts(self):
         """Whether draft steps run here: with draft weights, and not behind a prefix without draft keys."""
@@ -654,15 +661,16 @@ class Engine:
         max_k+1 tokens run sf_verify_step, sf_accept_commit and sf_draft_step over the whole batch.  A longer block runs
         on a helper engine created for that block length (same weights, same caches): one sf_prefill_step per block over
         the prompts that have started, or, where a prompt is empty, the three steps over the whole batch; its final lengths,
-        pending tokens and newest hooked rows are then handed to this engine.  Returns the first emitted token of every
-        sequence (device)."""
+        pending tokens and newest hooked rows are then handed to this engine.  Behind a shared prefix the prompts are the
+        sequences' tails; one that is empty begins behind the prefix.  Returns the first emitted token of every sequence
+        (device)."""
         q = self.max_k + 1 if block is None else int(block)
         if q <= self.max_k + 1:
             return _prefill_blocks(self, prompts, q, self.max_k)
         helper = Engine(self.cfg, self.B, self.cap, q - 1, device=self.dev, share_caches=self)
         helper.bind_shared(self, with_draft=self._D is not None)
         if self._prefix is not None:
-            helper._put_prefix(self._prefix.one, self._prefix.length, self._prefix.drafted)
+            helper._put_prefix(*self._prefix[:4])
         # row j of the helper is prompt order[j]; its K/V stay in the prompt's own cache slot
         lens = [len(p) for p in prompts]
         if len(lens) == self.B and min(lens) > 0:
@@ -757,4 +765,6 @@ def _prefill_blocks(eng, prompts, q, k_draft):
         eng.len_upper = int(done.max())
         if k_draft > 0 and eng._drafts():
             eng.sf_draft_step(k_draft)
+    if eng._prefix is not None and eng._prefix.start is not None and (lens == 0).any():
+        eng._start_behind_prefix(torch.from_numpy(np.flatnonzero(lens == 0)).to(eng.dev))
     return eng.pending.clone()

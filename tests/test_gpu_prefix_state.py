@@ -1,4 +1,5 @@
-"""What a context and an engine know about a shared prefix: calls in another order, a prefix whose draft keys are not there."""
+"""What a context and an engine know about a shared prefix: calls in another order, a prefix whose draft keys are not there,
+sequences without a tail."""
 import pytest
 import torch
 
@@ -108,3 +109,27 @@ def test_a_prefix_without_draft_keys(name):
             assert torch.equal(eng.prefill(tails, block=block), ref.prefill(tails, block=block)), what
             a, b = (x.sf_verify_step(k, draft)[0] for x in (eng, ref))
             assert torch.equal(a, b), what
+
+
+@pytest.mark.parametrize("block", [None, 8])
+def test_sequences_without_a_tail(block):
+    """A sequence whose tail is empty goes on right behind the prefix, as one that was not prefilled at all."""
+    k, seed, B = 3, 11, 3
+    shape, tw, dw = weights("8b-slice", k, seed)
+    one, eng, ref = Engine(shape.cfg(), 1, 64, k), Engine(shape.cfg(), B, 64, k), Engine(shape.cfg(), B, 64, k)
+    for e in (one, eng, ref):
+        e.bind(tw, dw)
+    one.prefill(synth.prompts([33], shape.vocab, seed))
+    for e in (eng, ref):
+        e.sf_set_prefix(one)
+    tails = synth.prompts([9, 20], shape.vocab, seed + 1)
+    first = eng.prefill([tails[0], tails[0][:0], tails[1]], block=block)
+    assert eng.kv_len.tolist() == [9, 0, 20] and eng.n_new[1] == 1 and first[1] == one.pending[0] == eng.pending[1]
+    assert torch.equal(eng.hooks[1, 0], ref.hooks[1, 0])
+    a, b = (logits_of_a_draft(e, k)[1] for e in (eng, ref))
+    assert torch.equal(a, b)
+    draft = torch.ones(B, k, dtype=torch.int32, device="cuda")
+    a, b = (e.sf_verify_step(k, draft)[0][1] for e in (eng, ref))
+    assert torch.equal(a, b)
+    eng.prefill([tails[0][:0]] * B, block=block)             # all of them
+    assert eng.kv_len.tolist() == [0] * B and eng.pending.tolist() == one.pending.tolist() * B

@@ -31,7 +31,7 @@ def _stream_addr():
 
 # What the sequences of an engine continue: the engine that holds it, its positions, whether their draft keys are there, the
 # pending token and newest hooked row behind them (None: the prefix is a part of what the engine holds).
-_Prefix = collections.namedtuple("_Prefix", "one length drafted start workspace")
+_Prefix = collections.namedtuple("_Prefix", "one length drafted start")
 
 
 class Engine:
@@ -84,6 +84,7 @@ class Engine:
                             _ptr(self.cu_new), C.c_void_p(self._ws_ptr), wb)
         self.len_upper = 0          # host-side upper bound of max_b kv_len[b]
         self._prefix = None
+        self._prefix_ws = None      # kept while the engine lives: steps may still run when a prefix goes
         self._pinned = False
         self._D = None
         self._undrafted = 0         # blocks committed since the draft step that last wrote draft keys (2: some are lost)
@@ -309,11 +310,13 @@ class Engine:
 
     def _put_prefix(self, one, length, drafted, start):
         nb = self.lib.sf_prefix_workspace_bytes(self.ctx, self.B, self.max_k, self.cap)
-        ws, at = self._workspace(nb)
+        if self._prefix_ws is None:
+            self._prefix_ws = self._workspace(nb)
+        at = self._prefix_ws[1]
         dk, dv = (one.dk, one.dv) if drafted else (None, None)
         pre = sfb.Prefix(length, one.cap, _addr(one.tk), _addr(one.tv), _addr(dk), _addr(dv), at if nb else None, nb)
         sfb.check(self.lib.sf_set_prefix(self.ctx, C.byref(pre)), "sf_set_prefix", self.ctx)
-        self._prefix = _Prefix(one, length, drafted, start, ws)
+        self._prefix = _Prefix(one, length, drafted, start)
 
     def _drafts(self):
         """Whether draft steps run here: with draft weights, and not behind a prefix without draft keys."""
@@ -670,7 +673,7 @@ class Engine:
         helper = Engine(self.cfg, self.B, self.cap, q - 1, device=self.dev, share_caches=self)
         helper.bind_shared(self, with_draft=self._D is not None)
         if self._prefix is not None:
-            helper._put_prefix(*self._prefix[:4])
+            helper._put_prefix(*self._prefix)
         # row j of the helper is prompt order[j]; its K/V stay in the prompt's own cache slot
         lens = [len(p) for p in prompts]
         if len(lens) == self.B and min(lens) > 0:

@@ -1,5 +1,5 @@
 """What a context and an engine know about a shared prefix: calls in another order, a prefix whose draft keys are not there,
-sequences without a tail."""
+sequences without a tail, memory that the steps still use."""
 import pytest
 import torch
 
@@ -133,3 +133,31 @@ def test_sequences_without_a_tail(block):
     assert torch.equal(a, b)
     eng.prefill([tails[0][:0]] * B, block=block)             # all of them
     assert eng.kv_len.tolist() == [0] * B and eng.pending.tolist() == one.pending.tolist() * B
+
+
+def test_the_steps_workspace_outlives_the_prefix():
+    """Steps may still run, on a stream of their own, when the prefix is taken away: their workspace is not given to others."""
+    k, seed, B = 3, 13, 4
+    shape, tw, dw = weights("8b-slice", k, seed)
+    one, eng = Engine(shape.cfg(), 1, 2048, k), Engine(shape.cfg(), B, 64, k)
+    for e in (one, eng):
+        e.bind(tw, dw)
+    one.prefill(synth.prompts([1500], shape.vocab, seed), block=64)
+    eng.sf_set_prefix(one)
+    n = eng.lib.sf_prefix_workspace_bytes(eng.ctx, B, k, 64) + 256
+    draft = torch.ones(B, k, dtype=torch.int32, device="cuda")
+    want = eng.sf_verify_step(k, draft)[0].clone()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = torch.empty_like(want)
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+        eng.sf_verify_step(k, draft, logits_out=got)
+        eng.sf_verify_step(k, draft, logits_out=got)
+    eng.sf_set_prefix(None)
+    others = [torch.full((n,), 0x7f, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    for _ in range(200):
+        for x in others:
+            x.fill_(0x7f)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)

@@ -143,7 +143,9 @@ size_t sf_kv_cache_bytes(const sf_ctx *ctx, int32_t which, int32_t B, int32_t ca
 sf_status sf_bind(sf_ctx *ctx, const sf_target_weights *target, const sf_draft_weights *draft);
 
 /* A prefix that all sequences of a context's later steps continue (several continuations of one prompt): its keys and values,
- * computed once, stand in front of every sequence and are read once per layer for all of them.  Positions count from its start:
+ * computed once, stand in front of every sequence (SF_BF16: a layer reads them once for every 128 query rows of a kv head, of
+ * whatever sequences; SF_F32: once for every row and head).  A row's logits do not depend on the block that it is verified in.
+ * Positions count from its start:
  * kv_len[b] (and host_len_upper, cap) are a sequence's own keys, its row i sits at position len + kv_len[b] + i.
  *   tk, tv  caches of ONE sequence of capacity cap (multiple of 32), as a state of B = 1 has them after a prefill of the prefix
  *   dk, dv  its draft caches, with the keys of all len positions (a block's are written by the draft step after its commit);
@@ -239,8 +241,8 @@ sf_status sf_op_attention(const sf_ctx *ctx, const void *q, const void *kc, cons
                           void *stream);
 
 /* Attention of a batch whose sequences all continue one shared prefix (several continuations of one prompt): row (b,i) sees
- * the prefix's keys [0, prefix_len), then what sf_op_attention would show it.  The prefix is read once for the rows of all
- * sequences, not once per sequence.
+ * the prefix's keys [0, prefix_len), then what sf_op_attention would show it.  SF_BF16: the prefix is read once for every
+ * 128 query rows of a kv head, of whatever sequences; SF_F32: once for every row and head.
  *   pk, pv      one layer's tiled caches of ONE sequence of capacity prefix_cap (multiple of 32), the slab that a state of
  *               B = 1 has; read only, what lies behind prefix_len is not looked at.  prefix_len: host, 0: sf_op_attention
  *   kc, vc      the sequences' own caches: positions behind the prefix, own key j of sequence b at slot j; kv_len[b] own keys
@@ -382,7 +384,9 @@ sf_status sf_op_accept(const sf_ctx *ctx, int32_t B, int32_t k, const int32_t *d
  *   min_p        of those, the ones with w_i >= min_p; <= 0 or NaN: all
  * The first of the ranking always stays; -inf has weight 0.  A token is drawn by a number u in [0, 1): the first, by index,
  * whose running kept weight exceeds u times the kept weight (u outside [0, 1) counts as the nearest border, NaN as the
- * upper one).  Weights and sums are doubles and their order is fixed: the same call returns the same bits. */
+ * upper one).  Weights are doubles, each to 2^-50, and sums have a fixed order or are whole numbers: the same call returns the same
+ * bits.  Where top_p filters without a top_k, weights are summed in multiples of 2^-36 of a bucket's edge: the border, the kept weight and
+ * what is derived from them (a draw's borders, prob, acceptance) are off by less than 2^-33 of the kept weight. */
 typedef struct {
   const float *temperature;
   const int32_t *top_k;

@@ -20,9 +20,9 @@ constexpr int STEP_TILES = 2;  // 32-key tiles between two meetings of a workgro
 typedef __amdgpu_buffer_rsrc_t buffer_t;
 #endif
 
-// Both parts for 128 x 5 rows of 40 / 8 heads of 128 over 8192 keys and 32 to 512 own ones take 147 us, 0.75 PFLOP/s: the
-// matrix instructions of a step and the exponentials between them do not overlap within a wave, and two waves to a SIMD fill a part
-// of each other's gaps.  64 rows to a wave, which halves the LDS reads, take 200 (registers); the small batches are latency: 32 x 5
+// Both parts for 128 x 5 rows of 40 / 8 heads of 128 over 8192 keys and 32 to 512 own ones take 144 us, 0.77 PFLOP/s (138
+// in a step, with the rotation and the append): the matrix instructions of a stage and the exponentials between them do not overlap
+// within a wave, and two waves to a SIMD fill a part of each other's gaps.  64 rows to a wave, which halves the LDS reads, take 200 (registers); the small batches are latency: 32 x 5
 // rows over 2048 keys of heads of 64 13 us.
 //
 // One workgroup: 128 rows of one kv head, chunk_tiles tiles of the prefix.  The cache's tiles are MFMA operands as they are: they

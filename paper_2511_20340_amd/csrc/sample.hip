@@ -7,11 +7,11 @@
 // its last element (thr, last): a token is kept if l > thr, or l == thr and its index <= last.  The token is the first, by
 // index, whose running kept weight exceeds u times the kept weight.
 //
-// Two launches, so that the logits leave memory once.  segment_kernel holds 8192 tokens of a row in the registers of a
+// Two launches, so that most of the logits leave memory once.  segment_kernel holds 8192 tokens of a row in the registers of a
 // workgroup and leaves what the row needs of them: the largest, the sum of weights, a histogram of weights (nucleus), the
 // tokens that may lie in the kept prefix.  row_kernel joins the segments, finds the prefix, finds the segment that u falls
 // into by the segments' kept weights, and reads that one again for the token.  What a segment had no room for (a flat row's
-// nucleus of tens of thousands) is read from the logits again, for that row alone.
+// nucleus of tens of thousands, a count behind a lead of more than 32) is read from the logits again, for that row alone.
 //
 // What bounds them: the first launch the vector instructions, at half the rate that the logits could be read with when all
 // rows ask for a nucleus (640 rows of 152064: 127 us, 3.1 TB/s) and 3.3 TB/s for settings of all kinds (256 of 128256: 40 us);
@@ -21,7 +21,9 @@
 // Weights are doubles: in a vocabulary of 150000 tokens a float sum is off by more than many tokens weigh, and the token
 // next to a border would hang on the order of the sum.  Where weights are summed by atomics they are integers (multiples of
 // 2^-62 in two halves, or of 2^-36 of a bucket's edge), so that the order does not matter there either: a row's result has the
-// same bits on every run.
+// same bits on every run.  A nucleus takes the bins' rounding: a token weighs e^-1/8 of its edge at least, so its sums are off by
+// 2^-36.8 of themselves, and the segments' shares, cut to 2^-49 in each of up to 128 x 255 bins, by 2^-34 together: less than 2^-33
+// of the kept weight, which is 1 at least.
 #include "sf_internal.h"
 #include <float.h>
 #include <limits.h>

@@ -265,7 +265,8 @@ class Engine:
         of the same shapes with B = 1, has in its caches.  start: begin behind them, no keys of their own yet, with one's pending
         token and newest hooked row.  one=None: no prefix any more.  The draft keys of a block that `one` has committed since its
         last draft step are written here (by a draft step of one).  Where they can not be, as `one` has no draft weights or has
-        committed several blocks without a draft step, sf_draft_step is refused (SF_ESTATE) behind this prefix."""
+        committed several blocks without a draft step, sf_draft_step is refused (SF_ESTATE) behind this prefix.  Blocks are
+        counted by one's calls: not the replays of a graph, and set_state with kv_len says that the caches hold what they should."""
         if one is None:
             sfb.check(self.lib.sf_set_prefix(self.ctx, None), "sf_set_prefix", self.ctx)
             self._prefix = None
